@@ -42,7 +42,7 @@
 extern "C" {
 #endif
 
-#define ILW_ABI_VERSION 9
+#define ILW_ABI_VERSION 10
 
 typedef enum {
   ILW_OK = 0,
@@ -413,10 +413,142 @@ int ilw_decoder_layer(const ilw_decoder_params* p, const int8_t* tgt, const int8
                       void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Keys and values kept between calls: a paged int8 cache with one scale for
+ * each page and kv head, for decoders that produce their tokens one after
+ * another.  A page holds page_size tokens of every kv head; a sequence's
+ * tokens 0, 1, ... lie in the pages its row of page_table names, in order.
+ *   k        int8 [n_pages, kv_heads, page_size, head_dim]
+ *   v        int8, as many bytes; within a page and head the tokens go in
+ *            groups of G = min(page_size, 64) (G * head_dim bytes each), and
+ *            channel c of token j of a group is its byte
+ *              (c/16)*16*G + ((j%16)/4)*4*G + (c%16)*(G/4) + (j/16)*4 + j%4
+ *            (four tokens of a channel are a word: the order in which the
+ *            attention's second product takes them)
+ *   k_scale, v_scale  int32 [n_pages, kv_heads]: a code c stands for
+ *            c * scale / 2^14 in units of the tensor it came from
+ *   page_table  int32 [sequences, max_pages], page numbers below n_pages.  A
+ *            number out of range is a page that is not there: tokens appended
+ *            to it are dropped, and attention sees no keys in it.
+ * All are DEVICE pointers, k and v 16-byte aligned; page_size 16, 32, 64, 128
+ * or 256; head_dim 32, 64, 128 or 256; max_pages * page_size <= 2^20.  The struct
+ * is read during the call.  Two sequences may share pages that neither
+ * appends to; a page that one call appends to belongs to one sequence of it.
+ */
+typedef struct {
+  int8_t* k;
+  int8_t* v;
+  int32_t* k_scale;
+  int32_t* v_scale;
+  const int32_t* page_table;
+  int32_t n_pages, page_size, max_pages, kv_heads, head_dim;
+} ilw_kv_cache;
+
+/* Appends the new tokens of `seqs` sequences to the cache and leaves their
+ * queries ready for ilw_cache_attention, queries and keys rotated by position
+ * on the way.
+ *   qkv      int8 [tokens, heads + 2*kv_heads, head_dim] (q | k | v, the output
+ *            of the QKV linear), rows ld bytes apart (ld >= a row, a multiple
+ *            of 16; 16-byte aligned)
+ *   cu_new   int32 [seqs + 1]: sequence s has rows cu_new[s] .. cu_new[s+1] - 1
+ *   past     int32 [seqs]: tokens of s already in the cache; the new ones are
+ *            tokens past[s], past[s] + 1, ... , which is also their position
+ *   rope     int16 [rope_rows, rotary_dim/2, 2]: cosine and sine of each
+ *            position, Q14, in [-2^14, 2^14]; 16-byte aligned; rope_rows at
+ *            least max_pages * page_size.  Ignored where rotary_dim is 0.
+ *   rotary_dim   channels 0 .. rotary_dim - 1 of a head are rotated, a multiple
+ *            of 16 up to head_dim; pair i is channels i and i + rotary_dim/2, or
+ *            2i and 2i + 1 with interleaved = 1
+ *   q        int8 [tokens, heads, head_dim], q_scale int32 [tokens, heads]
+ * Values, in Q14 of the QKV tensor's unit: x1 cos - x2 sin and x2 cos + x1 sin
+ * for a pair, x * 2^14 for other channels and for v.  With A the largest
+ * magnitude in a query head of a token, or in the call's new rows of a (page,
+ * kv head), need = max(1, ceil(A / 127)).  A query's scale is need, and so is a
+ * page's whose first slot is among the new rows.  Another page keeps its scale
+ * S if need <= S; else it takes S' = max(need, S + floor(S/8)) and its codes c
+ * become floor((2 c S + S') / (2 S')).  (The eighth bounds what a page filled
+ * token by token loses to repeated rounding: a scale grows at least
+ * geometrically, so the half steps lost sum to less than five of the last.)
+ * A value becomes the code floor((2 value + S) / (2 S)), in [-127, 127].
+ * Sequences longer than max_new new tokens, and tokens past max_pages *
+ * page_size or in pages that are not there, are not appended beyond those
+ * limits; query rows are written for the first max_new tokens of each
+ * sequence.  Rows outside every sequence are left as they are.  tokens and
+ * seqs may be 0.  One launch; no workspace.
+ */
+int ilw_cache_append(const ilw_kv_cache* cache, const int8_t* qkv, int64_t ld,
+                     const int32_t* cu_new, const int32_t* past, const int16_t* rope,
+                     int32_t rope_rows, int32_t rotary_dim, int32_t interleaved, int8_t* q,
+                     int32_t* q_scale, int32_t tokens, int32_t seqs, int32_t max_new,
+                     int32_t heads, void* stream);
+
+/* Attention of queries over the cache.  Sequence s has queries cu_q[s] ..
+ * cu_q[s+1] - 1 and lens[s] keys; with causal = 1 its queries are its last
+ * tokens, i.e. query i of n sees keys 0 .. lens[s] - n + i, of which only the
+ * last `window` ones if window > 0; with causal = 0 every query sees every key.
+ * heads is a multiple of kv_heads: query head h reads kv head h / (heads /
+ * kv_heads).
+ *   q int8, q_scale int32: as ilw_cache_append writes them; out int8 [tokens,
+ *   heads, head_dim] (all 16-byte aligned, contiguous)
+ * Integers throughout, with query scale Sq and the page's scales Sk and Sv:
+ *   A = (Sq * score_mult + 2^(t-1)) >> t,  t = score_shift - 16
+ *   s = clamp((q.k * ((A Sk + 2^15) >> 16) + 2^27) >> 28, +-32767)
+ *       a score in 1/64 octave: score_mult / 2^score_shift folds the tensors'
+ *       units, 1/sqrt(head_dim), log2(e) and 64
+ *   w = ((64 + f) << 16) >> (n + 6),  a = max s - s, n = ceil(a/64), f = 64 n - a
+ *       ShiftExp's chord of 2^(16 - a/64) (Sec. 3.3), max over the seen keys
+ *   L = sum w,  T = sum v * ((w Sv + 2^15) >> 16), exactly
+ *       each page's part at its own scale, brought to the common one as the
+ *       split convolution's branches are (Sec. 3.2.2)
+ *   d = bit length of L, - 16;  F = floor((2^31 - 1) / (L >> d))
+ *   out = sat8(rq((T F) >> (d + 13); out_mult, out_shift))
+ *       rq's input is the attention value in 2^-16 of the value tensor's unit
+ * Normalizing once, after the sum, keeps rows of 10^5 keys as exact as short
+ * ones, where int8 probabilities would round to 0.  A query that sees no key
+ * gives 0.  score_mult in [0, 2^31), score_shift in [17, 62] with 33026 *
+ * score_mult / 2^(score_shift - 16) < 2^31; out_shift in [1, 62].
+ * max_q and max_len bound the sequences' queries and keys: queries past max_q
+ * are left out (their rows untouched, as rows outside every sequence are), keys
+ * past max_len are not there.  max_len <= max_pages * page_size.
+ * q_scale in [1, 33026], page scales in [1, 37154] (keys) and [1, 18577]
+ * (values), which ilw_cache_append keeps to.  The workspace may hold anything.
+ */
+typedef struct {
+  int32_t score_mult, score_shift;
+  int32_t out_mult, out_shift;
+  int32_t causal, window;
+} ilw_cache_attn_params;
+
+size_t ilw_cache_attention_workspace_bytes(const ilw_kv_cache* cache, int32_t seqs,
+                                           int32_t max_q, int32_t max_len, int32_t heads);
+int ilw_cache_attention(const ilw_kv_cache* cache, const int8_t* q, const int32_t* q_scale,
+                        const int32_t* cu_q, const int32_t* lens, int8_t* out,
+                        int32_t tokens, int32_t seqs, int32_t max_q, int32_t max_len,
+                        int32_t heads, const ilw_cache_attn_params* ap, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Linear layers of several experts over rows sorted by expert: ilw_linear with
+ * expert e's weights for rows offsets[e] .. offsets[e+1] - 1 (Sec. 3.2.1).
+ *   y[m][n] = sat8(rq(b[e][n] + sum_k x[r][k] * w[e][n][k]; rq[e][n]))
+ *   x        int8 [x_rows, K];  r = m, or rows[m] where rows is not NULL
+ *            (DEVICE int32 [M]; an r outside [0, x_rows) reads a row of zeros)
+ *   offsets  DEVICE int32 [experts + 1], not decreasing, in [0, M]; rows of y
+ *            outside [offsets[0], offsets[experts]) are left as they are
+ *   w int8 [experts, N, K], b int32 [experts, N] or NULL, y int8 [M, N]
+ *   rq       n = 1 (one factor for all) or experts * N
+ * N and K multiples of 16, K <= 131072, experts in [1, 1024]; x and w 16-byte
+ * aligned, y 4-byte aligned and not aliasing x.  M == 0 is a no-op.
+ */
+int ilw_linear_grouped(const int8_t* x, int64_t x_rows, const int32_t* rows,
+                       const int32_t* offsets, const int8_t* w, const int32_t* b,
+                       ilw_dyadic rq, int8_t* y, int64_t M, int32_t experts, int32_t N,
+                       int32_t K, void* stream);
+
+/* ------------------------------------------------------------------------
  * Per-stage kernel timing (tracing; off by default).  While enabled, every
  * kernel that ilw_block_forward, ilw_encoder_forward, ilw_attention,
- * ilw_deform_attn, ilw_split_conv, ilw_patch_embed and ilw_decoder_layer
- * launch is bracketed by a pair of HIP events recorded on the
+ * ilw_deform_attn, ilw_split_conv, ilw_patch_embed, ilw_decoder_layer,
+ * ilw_cache_append, ilw_cache_attention and ilw_linear_grouped launch is bracketed by a pair of HIP events recorded on the
  * caller's stream, and the launch is attributed to one of the stages below.
  * Enabling (or disabling)
  * clears the records.  ilw_profile_read waits for the last recorded event and
@@ -440,7 +572,10 @@ typedef enum {
   ILW_STAGE_DECODER = 11,    /* decoder linears, LayerNorms, offset widening */
   ILW_STAGE_TAIL384 = 12,    /* projection ... fc2 + residual (+ next LN1),
                                 one launch (dim 384)                        */
-  ILW_NUM_STAGES = 13
+  ILW_STAGE_CACHE_APPEND = 13, /* rotation and append to the paged cache    */
+  ILW_STAGE_CACHE_ATTENTION = 14, /* attention over the paged cache         */
+  ILW_STAGE_GEMM_GROUPED = 15, /* linears grouped by expert                 */
+  ILW_NUM_STAGES = 16
 } ilw_stage;
 
 int ilw_profile_enable(int enable);

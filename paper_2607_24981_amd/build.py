@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 SO = os.path.join(HERE, "libilw.so")
 SOURCES = ["api.hip", "gemm.hip", "ln_gemm.hip", "tail384.hip", "attention.hip", "rowops.hip",
-           "deform.hip", "block_tail.hip", "split_conv.hip"]
+           "deform.hip", "block_tail.hip", "split_conv.hip", "cache_append.hip",
+           "cache_attention.hip", "grouped.hip"]
 ARCH = "gfx950"
 
 

@@ -806,6 +806,56 @@ int check_decoder(const ilw_decoder_params* p, int32_t batch, int32_t Q, int32_t
   return ILW_OK;
 }
 
+// A paged cache as the kernels take it.
+int check_cache(const ilw_kv_cache* c, int32_t seqs, CacheView* v) {
+  REQUIRE(c, ILW_E_NULL, "the cache must not be NULL");
+  const int32_t P = c->page_size, D = c->head_dim;
+  REQUIRE(P == 16 || P == 32 || P == 64 || P == 128 || P == 256, ILW_E_UNSUPPORTED,
+          "page_size = %d: 16, 32, 64, 128 and 256 are implemented", P);
+  REQUIRE(D == 32 || D == 64 || D == 128 || D == 256, ILW_E_UNSUPPORTED,
+          "head_dim = %d: 32, 64, 128 and 256 are implemented", D);
+  REQUIRE(c->kv_heads >= 1 && c->kv_heads <= 4096, ILW_E_SHAPE,
+          "kv_heads = %d must be in [1, 4096]", c->kv_heads);
+  REQUIRE(c->n_pages >= 1 && c->max_pages >= 1, ILW_E_SHAPE,
+          "n_pages = %d and max_pages = %d must be positive", c->n_pages, c->max_pages);
+  REQUIRE((int64_t)c->max_pages * P <= (1 << 20), ILW_E_UNSUPPORTED,
+          "max_pages * page_size = %lld must be at most 2^20", (long long)c->max_pages * P);
+  REQUIRE((int64_t)c->n_pages * c->kv_heads < ((int64_t)1 << 31), ILW_E_UNSUPPORTED,
+          "n_pages * kv_heads = %lld must be below 2^31", (long long)c->n_pages * c->kv_heads);
+  REQUIRE(seqs >= 0 && seqs <= 65535, ILW_E_SHAPE, "seqs = %d must be in [0, 65535]", seqs);
+  if (seqs > 0) {
+    REQUIRE(c->k && c->v && c->k_scale && c->v_scale && c->page_table, ILW_E_NULL,
+            "the cache's pointers must not be NULL");
+    REQUIRE(aligned16(c->k) && aligned16(c->v), ILW_E_PARAM, "k and v must be 16-byte aligned");
+  }
+  v->k = c->k;
+  v->v = c->v;
+  v->k_scale = c->k_scale;
+  v->v_scale = c->v_scale;
+  v->table = c->page_table;
+  v->n_pages = c->n_pages;
+  v->max_pages = c->max_pages;
+  v->Hkv = c->kv_heads;
+  v->D = D;
+  v->lp = __builtin_ctz((unsigned)P);
+  return ILW_OK;
+}
+
+int check_cache_attention(const CacheView& c, int32_t seqs, int32_t max_q, int32_t max_len,
+                          int32_t heads) {
+  REQUIRE(heads >= c.Hkv && heads <= 4096 && heads % c.Hkv == 0, ILW_E_SHAPE,
+          "heads = %d must be a multiple of kv_heads = %d, at most 4096", heads, c.Hkv);
+  REQUIRE(max_q >= 0 && max_q <= (1 << 20), ILW_E_SHAPE, "max_q = %d must be in [0, 2^20]", max_q);
+  REQUIRE(max_len >= 0 && max_len <= (c.max_pages << c.lp), ILW_E_SHAPE,
+          "max_len = %d must be in [0, max_pages * page_size = %d]", max_len,
+          c.max_pages << c.lp);
+  REQUIRE((int64_t)max_q * (heads / c.Hkv) <= (1 << 24) &&
+              ((int64_t)max_q * (heads / c.Hkv) + 15) / 16 * seqs * c.Hkv < ((int64_t)1 << 28),
+          ILW_E_UNSUPPORTED, "too many query rows: max_q = %d, heads = %d, seqs = %d", max_q,
+          heads, seqs);
+  return ILW_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1383,6 +1433,172 @@ int ilw_decoder_layer(const ilw_decoder_params* p, const int8_t* tgt, const int8
   resid_ln(gemm_args(L.g, p->w_fc2, p->b_fc2, p->fc2, L.x, MQ, D, F), L.t2, p->res3_mult_a,
            p->res3_mult_b, p->res3_shift, p->ln3_beta, p->ln3_out, y);
   return hip_status(he, "ilw_decoder_layer");
+}
+
+size_t ilw_cache_attention_workspace_bytes(const ilw_kv_cache* cache, int32_t seqs,
+                                           int32_t max_q, int32_t max_len, int32_t heads) {
+  CacheAttnArgs a = {};
+  if (check_cache(cache, seqs, &a.c) || check_cache_attention(a.c, seqs, max_q, max_len, heads))
+    return 0;
+  a.seqs = seqs;
+  a.max_q = max_q;
+  a.max_len = max_len;
+  a.Hq = heads;
+  ok();
+  return cache_attention_workspace(a);
+}
+
+int ilw_cache_append(const ilw_kv_cache* cache, const int8_t* qkv, int64_t ld,
+                     const int32_t* cu_new, const int32_t* past, const int16_t* rope,
+                     int32_t rope_rows, int32_t rotary_dim, int32_t interleaved, int8_t* q,
+                     int32_t* q_scale, int32_t tokens, int32_t seqs, int32_t max_new,
+                     int32_t heads, void* stream) {
+  AppendArgs a = {};
+  int e;
+  if ((e = check_cache(cache, seqs, &a.c))) return e;
+  REQUIRE(tokens >= 0 && max_new >= 0, ILW_E_SHAPE, "tokens = %d and max_new = %d must be >= 0",
+          tokens, max_new);
+  REQUIRE(heads >= 1 && heads <= 4096, ILW_E_SHAPE, "heads = %d must be in [1, 4096]", heads);
+  const int64_t row = ((int64_t)heads + 2 * cache->kv_heads) * cache->head_dim;
+  REQUIRE(ld >= row && ld % 16 == 0, ILW_E_SHAPE,
+          "ld = %lld must be a multiple of 16 and at least %lld, a row of q | k | v", (long long)ld,
+          (long long)row);
+  REQUIRE(rotary_dim >= 0 && rotary_dim <= cache->head_dim && rotary_dim % 16 == 0, ILW_E_SHAPE,
+          "rotary_dim = %d must be a multiple of 16 up to head_dim = %d", rotary_dim,
+          cache->head_dim);
+  REQUIRE(interleaved == 0 || interleaved == 1, ILW_E_PARAM, "interleaved = %d must be 0 or 1",
+          interleaved);
+  REQUIRE(rotary_dim == 0 || rope_rows >= cache->max_pages * cache->page_size, ILW_E_SHAPE,
+          "rope_rows = %d must cover the %d positions of a sequence", rope_rows,
+          cache->max_pages * cache->page_size);
+  if (tokens == 0 || seqs == 0 || max_new == 0) return ok();
+  REQUIRE(qkv && cu_new && past && q && q_scale, ILW_E_NULL,
+          "qkv, cu_new, past, q and q_scale must not be NULL");
+  REQUIRE(rotary_dim == 0 || rope, ILW_E_NULL, "rope must not be NULL where rotary_dim > 0");
+  REQUIRE(aligned16(qkv) && aligned16(q) && (rotary_dim == 0 || aligned16(rope)), ILW_E_PARAM,
+          "qkv, q and rope must be 16-byte aligned");
+  a.qkv = qkv;
+  a.ld = ld;
+  a.cu = cu_new;
+  a.past = past;
+  a.rope = rope;
+  a.R = rotary_dim;
+  a.inter = interleaved;
+  a.q = q;
+  a.q_scale = q_scale;
+  a.T = tokens;
+  a.seqs = seqs;
+  a.max_new = max_new < tokens ? max_new : tokens;
+  a.Hq = heads;
+  hipStream_t s = (hipStream_t)stream;
+  StageTimer t(ILW_STAGE_CACHE_APPEND, s);
+  const hipError_t he = launch_cache_append(a, s);
+  t.done();
+  return hip_status(he, "ilw_cache_append");
+}
+
+int ilw_cache_attention(const ilw_kv_cache* cache, const int8_t* q, const int32_t* q_scale,
+                        const int32_t* cu_q, const int32_t* lens, int8_t* out,
+                        int32_t tokens, int32_t seqs, int32_t max_q, int32_t max_len,
+                        int32_t heads, const ilw_cache_attn_params* ap, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  CacheAttnArgs a = {};
+  int e;
+  if ((e = check_cache(cache, seqs, &a.c))) return e;
+  if ((e = check_cache_attention(a.c, seqs, max_q, max_len, heads))) return e;
+  REQUIRE(tokens >= 0, ILW_E_SHAPE, "tokens = %d must be >= 0", tokens);
+  REQUIRE(ap, ILW_E_NULL, "attention parameters must not be NULL");
+  REQUIRE(ap->score_mult >= 0, ILW_E_PARAM, "score_mult = %d must be >= 0", ap->score_mult);
+  REQUIRE(ap->score_shift >= 17 && ap->score_shift <= 62, ILW_E_PARAM,
+          "score_shift = %d must be in [17, 62]", ap->score_shift);
+  REQUIRE((33026 * (int64_t)ap->score_mult + ((int64_t)1 << (ap->score_shift - 17))) >>
+                  (ap->score_shift - 16) < ((int64_t)1 << 31),
+          ILW_E_PARAM, "score_mult / 2^score_shift = %d / 2^%d is too large", ap->score_mult,
+          ap->score_shift);
+  if ((e = check_mult(ap->out_mult, "out_mult"))) return e;
+  if ((e = check_shift(ap->out_shift, "out_shift"))) return e;
+  REQUIRE(ap->causal == 0 || ap->causal == 1, ILW_E_PARAM, "causal = %d must be 0 or 1",
+          ap->causal);
+  REQUIRE(ap->window >= 0 && (ap->window == 0 || ap->causal), ILW_E_PARAM,
+          "window = %d must be >= 0, and 0 where causal is 0", ap->window);
+  if (tokens == 0 || seqs == 0 || max_q == 0) return ok();
+  REQUIRE(q && q_scale && cu_q && lens && out, ILW_E_NULL,
+          "q, q_scale, cu_q, lens and out must not be NULL");
+  REQUIRE(aligned16(q) && aligned16(out), ILW_E_PARAM, "q and out must be 16-byte aligned");
+  a.q = q;
+  a.q_scale = q_scale;
+  a.cu = cu_q;
+  a.lens = lens;
+  a.out = out;
+  a.T = tokens;
+  a.seqs = seqs;
+  a.max_q = max_q;
+  a.max_len = max_len;
+  a.Hq = heads;
+  a.score_mult = ap->score_mult;
+  a.score_t = ap->score_shift - 16;
+  a.out_mult = ap->out_mult;
+  a.out_shift = ap->out_shift;
+  a.causal = ap->causal;
+  a.window = ap->window;
+  const size_t need = cache_attention_workspace(a);
+  REQUIRE(need == 0 || (workspace && workspace_bytes >= need), ILW_E_WORKSPACE,
+          "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+  REQUIRE(aligned16(workspace), ILW_E_PARAM, "workspace must be 16-byte aligned");
+  hipStream_t s = (hipStream_t)stream;
+  StageTimer t(ILW_STAGE_CACHE_ATTENTION, s);
+  const hipError_t he = launch_cache_attention(a, workspace, s);
+  t.done();
+  return hip_status(he, "ilw_cache_attention");
+}
+
+int ilw_linear_grouped(const int8_t* x, int64_t x_rows, const int32_t* rows,
+                       const int32_t* offsets, const int8_t* w, const int32_t* b,
+                       ilw_dyadic rq, int8_t* y, int64_t M, int32_t experts, int32_t N,
+                       int32_t K, void* stream) {
+  REQUIRE(M >= 0 && x_rows >= 0 && N >= 16 && K >= 16, ILW_E_SHAPE,
+          "M=%lld x_rows=%lld N=%d K=%d invalid", (long long)M, (long long)x_rows, N, K);
+  REQUIRE(experts >= 1 && experts <= 1024, ILW_E_SHAPE, "experts = %d must be in [1, 1024]",
+          experts);
+  REQUIRE(N % 16 == 0 && K % 16 == 0, ILW_E_SHAPE, "N=%d and K=%d must be multiples of 16", N, K);
+  REQUIRE(K <= 131072, ILW_E_UNSUPPORTED, "K=%d: the int32 accumulator needs K <= 131072", K);
+  REQUIRE((int64_t)experts * N < ((int64_t)1 << 31), ILW_E_UNSUPPORTED,
+          "experts * N = %lld must be below 2^31", (long long)experts * N);
+  REQUIRE(M < ((int64_t)1 << 31) && x_rows < ((int64_t)1 << 31), ILW_E_UNSUPPORTED,
+          "M=%lld and x_rows=%lld must be below 2^31", (long long)M, (long long)x_rows);
+  REQUIRE((M / 16 + experts) * ((N + 63) / 64) < (int64_t)1 << 31, ILW_E_UNSUPPORTED,
+          "too many tiles");
+  REQUIRE(rows || x_rows >= M, ILW_E_SHAPE, "x has %lld rows, %lld needed", (long long)x_rows,
+          (long long)M);
+  if (M == 0) return ok();
+  REQUIRE(x_rows > 0, ILW_E_SHAPE, "x must have a row");
+  REQUIRE(x && w && y && offsets, ILW_E_NULL, "x, w, y and offsets must not be NULL");
+  REQUIRE(aligned16(x) && aligned16(w) && ((uintptr_t)y & 3) == 0, ILW_E_PARAM,
+          "x and w must be 16-byte aligned, y 4-byte aligned");
+  REQUIRE(rq.mult && rq.shift, ILW_E_NULL, "rq: mult/shift must not be NULL");
+  REQUIRE(rq.n == 1 || rq.n == experts * N, ILW_E_SHAPE,
+          "rq: n = %d must be 1 (one factor) or %d (one per expert and channel)", rq.n,
+          experts * N);
+  GroupedArgs a = {};
+  a.x = x;
+  a.rows = rows;
+  a.offsets = offsets;
+  a.w = w;
+  a.bias = b;
+  a.mult = rq.mult;
+  a.shift = rq.shift;
+  a.y = y;
+  a.M = M;
+  a.x_rows = x_rows;
+  a.nq = rq.n;
+  a.E = experts;
+  a.N = N;
+  a.K = K;
+  hipStream_t s = (hipStream_t)stream;
+  StageTimer t(ILW_STAGE_GEMM_GROUPED, s);
+  const hipError_t he = launch_grouped(a, s);
+  t.done();
+  return hip_status(he, "ilw_linear_grouped");
 }
 
 int ilw_profile_enable(int enable) {

@@ -18,7 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # ILW_LIBRARY_PATH loads another build of the same sources instead (the
 # sanitizer run of the CPU test-suite uses a host-instrumented one).
 LIB_PATH = os.environ.get("ILW_LIBRARY_PATH") or os.path.join(_HERE, "libilw.so")
-ABI_VERSION = 9
+ABI_VERSION = 10
 
 c_i32, c_i64, c_vp, c_size = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
 
@@ -35,6 +35,17 @@ class AttnParams(ctypes.Structure):
     _fields_ = [("score_mult", c_i32), ("score_shift", c_i32), ("I0", c_i32),
                 ("k_inter", c_i32), ("k_out", c_i32), ("m_p", c_i32), ("s_d", c_i32),
                 ("pv_mult", c_i32), ("pv_shift", c_i32)]
+
+
+class KVCacheStruct(ctypes.Structure):
+    _fields_ = ([(n, c_vp) for n in ("k", "v", "k_scale", "v_scale", "page_table")]
+                + [(n, c_i32) for n in ("n_pages", "page_size", "max_pages", "kv_heads",
+                                        "head_dim")])
+
+
+class CacheAttnParams(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("score_mult", "score_shift", "out_mult", "out_shift",
+                                     "causal", "window")]
 
 
 class BlockParams(ctypes.Structure):
@@ -113,6 +124,15 @@ _SIGS = {
                                              c_i32]),
     "ilw_decoder_layer": (ctypes.c_int, [ctypes.POINTER(DecoderParams), c_vp, c_vp, c_vp, c_vp,
                                          c_vp, c_vp, c_i32, c_i32, c_i32, c_vp, c_size, c_vp]),
+    "ilw_cache_append": (ctypes.c_int, [ctypes.POINTER(KVCacheStruct), c_vp, c_i64, c_vp, c_vp,
+                                        c_vp, c_i32, c_i32, c_i32, c_vp, c_vp] + [c_i32] * 4 +
+                         [c_vp]),
+    "ilw_cache_attention_workspace_bytes": (c_size, [ctypes.POINTER(KVCacheStruct)] +
+                                            [c_i32] * 4),
+    "ilw_cache_attention": (ctypes.c_int, [ctypes.POINTER(KVCacheStruct)] + [c_vp] * 5 +
+                            [c_i32] * 5 + [ctypes.POINTER(CacheAttnParams), c_vp, c_size, c_vp]),
+    "ilw_linear_grouped": (ctypes.c_int, [c_vp, c_i64, c_vp, c_vp, c_vp, c_vp, Dyadic, c_vp,
+                                          c_i64, c_i32, c_i32, c_i32, c_vp]),
     "ilw_profile_enable": (ctypes.c_int, [ctypes.c_int]),
     "ilw_profile_read": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double),
                                         ctypes.POINTER(c_i32), c_i32]),
@@ -576,8 +596,163 @@ def ilw_deform_attn_boxes(value, level_hw, level_start, ref, offsets, logits, I0
                    logits, I0, out_mult, out_shift, mode, s_d, out, k_inter, k_out, m_p)
 
 
+class KVCache:
+    """A paged int8 cache: pools k and v int8 [n_pages, kv_heads, page_size,
+    head_dim] (v's order within a page: see include/ilw.h), scales int32
+    [n_pages, kv_heads] and page_table int32 [sequences, max_pages].  The
+    tensors stay the caller's; appending changes them in place."""
+
+    def __init__(self, k, v, k_scale, v_scale, page_table):
+        if k.dim() != 4 or v.shape != k.shape:
+            raise IlwError("k and v must be [n_pages, kv_heads, page_size, head_dim], got "
+                           f"{tuple(k.shape)} and {tuple(v.shape)}")
+        n, h, p, d = k.shape
+        if tuple(k_scale.shape) != (n, h) or tuple(v_scale.shape) != (n, h):
+            raise IlwError(f"k_scale and v_scale must be {(n, h)}, got {tuple(k_scale.shape)} and "
+                           f"{tuple(v_scale.shape)}")
+        if page_table.dim() != 2:
+            raise IlwError("page_table must be [sequences, max_pages]")
+        _same_device(k, v, k_scale, v_scale, page_table)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.page_table = page_table
+        self.seqs = page_table.shape[0]
+        self.struct = KVCacheStruct(
+            _dev(k, torch.int8, "k"), _dev(v, torch.int8, "v"),
+            _dev(k_scale, torch.int32, "k_scale"), _dev(v_scale, torch.int32, "v_scale"),
+            _dev(page_table, torch.int32, "page_table"), n, p, page_table.shape[1], h, d)
+
+    @classmethod
+    def empty(cls, n_pages, kv_heads, page_size, head_dim, page_table):
+        """Fresh pools beside a page table."""
+        dev = page_table.device
+        k, v = (torch.zeros(n_pages, kv_heads, page_size, head_dim, dtype=torch.int8, device=dev)
+                for _ in range(2))
+        ks, vs = (torch.ones(n_pages, kv_heads, dtype=torch.int32, device=dev) for _ in range(2))
+        return cls(k, v, ks, vs, page_table)
+
+
+def _same_device(*tensors):
+    """Calls go to the current device's stream: every tensor has to be there."""
+    cur = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != cur:
+            raise IlwError(f"a tensor on {t.device}, with cuda:{cur} the current device")
+
+
+def _shape(t, shape, name):
+    if tuple(t.shape) != tuple(shape):
+        raise IlwError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def rope_table(rows, rotary_dim, base=10000.0, device="cuda"):
+    """Q14 cosines and sines int16 [rows, rotary_dim / 2, 2] of the positions
+    0 .. rows - 1, angles position * base^(-2 i / rotary_dim) in double."""
+    at = torch.arange(rows, dtype=torch.float64).view(-1, 1)
+    inv = base ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64) / rotary_dim)
+    a = at * inv
+    return torch.stack([a.cos(), a.sin()], -1).mul_(16384).round_().to(torch.int16).to(device)
+
+
+def ilw_cache_append(cache: KVCache, qkv, heads, cu_new, past, max_new, rope=None,
+                     interleaved=False, q=None, q_scale=None):
+    """qkv int8 [T, (heads + 2 kv_heads) * head_dim] (its rows may be strided);
+    cu_new int32 [seqs + 1], past int32 [seqs], rope int16 [rows, rotary / 2, 2]
+    or None (no rotation) -> q int8 [T, heads, head_dim], q_scale int32 [T,
+    heads]; keys and values go to the cache."""
+    c = cache.struct
+    T = qkv.shape[0]
+    if qkv.dim() != 2 or qkv.shape[1] != (heads + 2 * c.kv_heads) * c.head_dim:
+        raise IlwError(f"qkv must be [tokens, {(heads + 2 * c.kv_heads) * c.head_dim}], got "
+                       f"{tuple(qkv.shape)}")
+    if not qkv.is_cuda or qkv.dtype != torch.int8 or (T > 0 and qkv.stride(1) != 1):
+        raise IlwError("qkv must be an int8 device tensor with contiguous rows")
+    _shape(cu_new, (cache.seqs + 1,), "cu_new")
+    _shape(past, (cache.seqs,), "past")
+    if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2):
+        raise IlwError("rope must be [rows, rotary_dim / 2, 2]")
+    if q is None:
+        q = torch.empty((T, heads, c.head_dim), dtype=torch.int8, device=qkv.device)
+    if q_scale is None:
+        q_scale = torch.empty((T, heads), dtype=torch.int32, device=qkv.device)
+    _shape(q, (T, heads, c.head_dim), "q")
+    _shape(q_scale, (T, heads), "q_scale")
+    _same_device(cache.k, qkv, cu_new, past, rope, q, q_scale)
+    rc = lib().ilw_cache_append(
+        ctypes.byref(c), c_vp(qkv.data_ptr()), qkv.stride(0) if T > 1 else qkv.shape[1],
+        _dev(cu_new, torch.int32, "cu_new"), _dev(past, torch.int32, "past"),
+        None if rope is None else _dev(rope, torch.int16, "rope"),
+        0 if rope is None else rope.shape[0], 0 if rope is None else 2 * rope.shape[1],
+        int(interleaved), _dev(q, torch.int8, "q"), _dev(q_scale, torch.int32, "q_scale"), T,
+        cache.seqs, max_new, heads, _stream())
+    _check(rc, "ilw_cache_append")
+    return q, q_scale
+
+
+def ilw_cache_attention(cache: KVCache, q, q_scale, cu_q, lens, params: dict, max_q, max_len,
+                        causal=True, window=0, out=None, workspace=None):
+    """q int8 [T, heads, head_dim] and q_scale int32 [T, heads] over the cache's
+    first lens[s] tokens of each sequence -> int8 [T, heads * head_dim].  params:
+    score_mult, score_shift, out_mult, out_shift."""
+    c = cache.struct
+    if q.dim() != 3 or q.shape[2] != c.head_dim:
+        raise IlwError(f"q must be [tokens, heads, {c.head_dim}], got {tuple(q.shape)}")
+    T, heads, D = q.shape
+    _shape(q_scale, (T, heads), "q_scale")
+    _shape(cu_q, (cache.seqs + 1,), "cu_q")
+    _shape(lens, (cache.seqs,), "lens")
+    if out is None:
+        out = torch.empty((T, heads * D), dtype=torch.int8, device=q.device)
+    if out.numel() != T * heads * D:
+        raise IlwError(f"out must have {T * heads * D} elements, got {out.numel()}")
+    if workspace is None:
+        need = lib().ilw_cache_attention_workspace_bytes(ctypes.byref(c), cache.seqs, max_q,
+                                                         max_len, heads)
+        if need == 0 and last_error():
+            raise IlwError(f"ilw_cache_attention_workspace_bytes: {last_error()}")
+        workspace = torch.empty(max(need, 16), dtype=torch.int8, device=q.device)
+    _same_device(cache.k, q, q_scale, cu_q, lens, out, workspace)
+    ap = CacheAttnParams(int(params["score_mult"]), int(params["score_shift"]),
+                         int(params["out_mult"]), int(params["out_shift"]), int(causal),
+                         int(window))
+    rc = lib().ilw_cache_attention(
+        ctypes.byref(c), _dev(q, torch.int8, "q"), _dev(q_scale, torch.int32, "q_scale"),
+        _dev(cu_q, torch.int32, "cu_q"), _dev(lens, torch.int32, "lens"),
+        _dev(out, torch.int8, "out"), T, cache.seqs, max_q, max_len, heads, ctypes.byref(ap),
+        _dev(workspace, torch.int8, "workspace"), workspace.numel(), _stream())
+    _check(rc, "ilw_cache_attention")
+    return out
+
+
+def ilw_linear_grouped(x, w, offsets, b, mult, shift, rows=None, y=None):
+    """x int8 [R, K], w int8 [E, N, K], offsets int32 [E + 1], b int32 [E, N] or
+    None, mult and shift int32 [1] or [E, N], rows int32 [M] (row of x for each
+    row of y) or None (M = R) -> int8 [M, N]."""
+    E, N, K = w.shape
+    if x.dim() != 2 or x.shape[1] != K:
+        raise IlwError(f"x must be [rows, {K}], got {tuple(x.shape)}")
+    M = x.shape[0] if rows is None else rows.shape[0]
+    _shape(offsets, (E + 1,), "offsets")
+    if b is not None:
+        _shape(b, (E, N), "b")
+    if shift.numel() != mult.numel():
+        raise IlwError(f"mult and shift have {mult.numel()} and {shift.numel()} entries")
+    if y is None:
+        y = torch.empty((M, N), dtype=torch.int8, device=x.device)
+    _shape(y, (M, N), "y")
+    _same_device(x, w, offsets, b, mult, shift, rows, y)
+    rc = lib().ilw_linear_grouped(
+        _dev(x, torch.int8, "x"), x.shape[0],
+        None if rows is None else _dev(rows, torch.int32, "rows"),
+        _dev(offsets, torch.int32, "offsets"), _dev(w, torch.int8, "w"),
+        None if b is None else _dev(b, torch.int32, "b"), _dyadic(mult, shift),
+        _dev(y, torch.int8, "y"), M, E, N, K, _stream())
+    _check(rc, "ilw_linear_grouped")
+    return y
+
+
 STAGES = ["layernorm", "gemm_qkv", "attention", "gemm_proj", "gemm_fc1", "gemm_fc2",
-          "relayout", "deform", "block_tail", "split_conv", "patch_embed", "decoder", "tail384"]
+          "relayout", "deform", "block_tail", "split_conv", "patch_embed", "decoder", "tail384",
+          "cache_append", "cache_attention", "gemm_grouped"]
 
 
 def profile_enable(on: bool = True):
