@@ -596,6 +596,34 @@ def ilw_deform_attn_boxes(value, level_hw, level_start, ref, offsets, logits, I0
                    logits, I0, out_mult, out_shift, mode, s_d, out, k_inter, k_out, m_p)
 
 
+def _device(t, name) -> int:
+    """Index of the device that a call goes to: t's, which has to be the current
+    one (calls are issued on its current stream)."""
+    d = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if d < 0:
+        raise IlwError(f"{name} must be a device tensor")
+    if d != torch.cuda.current_device():
+        raise IlwError(f"{name} is on cuda:{d}, and cuda:{torch.cuda.current_device()} is the "
+                       "current device")
+    return d
+
+
+def _at(t, dtype, name, device) -> int:
+    """Address of a contiguous tensor of that type on that device."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        raise IlwError(f"{name} must be a tensor on cuda:{device}")
+    if t.dtype is not dtype:
+        raise IlwError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise IlwError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _shape(t, shape, name):
+    if t.shape != shape:
+        raise IlwError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+
+
 class KVCache:
     """A paged int8 cache: pools k and v int8 [n_pages, kv_heads, page_size,
     head_dim] (v's order within a page: see include/ilw.h), scales int32
@@ -603,23 +631,23 @@ class KVCache:
     tensors stay the caller's; appending changes them in place."""
 
     def __init__(self, k, v, k_scale, v_scale, page_table):
+        self.device = dev = _device(k, "k")
         if k.dim() != 4 or v.shape != k.shape:
             raise IlwError("k and v must be [n_pages, kv_heads, page_size, head_dim], got "
                            f"{tuple(k.shape)} and {tuple(v.shape)}")
         n, h, p, d = k.shape
-        if tuple(k_scale.shape) != (n, h) or tuple(v_scale.shape) != (n, h):
-            raise IlwError(f"k_scale and v_scale must be {(n, h)}, got {tuple(k_scale.shape)} and "
-                           f"{tuple(v_scale.shape)}")
+        _shape(k_scale, (n, h), "k_scale")
+        _shape(v_scale, (n, h), "v_scale")
         if page_table.dim() != 2:
             raise IlwError("page_table must be [sequences, max_pages]")
-        _same_device(k, v, k_scale, v_scale, page_table)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.page_table = page_table
-        self.seqs = page_table.shape[0]
+        self.seqs, pages = page_table.shape
+        self.kv_heads, self.page_size, self.head_dim = h, p, d
         self.struct = KVCacheStruct(
-            _dev(k, torch.int8, "k"), _dev(v, torch.int8, "v"),
-            _dev(k_scale, torch.int32, "k_scale"), _dev(v_scale, torch.int32, "v_scale"),
-            _dev(page_table, torch.int32, "page_table"), n, p, page_table.shape[1], h, d)
+            _at(k, torch.int8, "k", dev), _at(v, torch.int8, "v", dev),
+            _at(k_scale, torch.int32, "k_scale", dev), _at(v_scale, torch.int32, "v_scale", dev),
+            _at(page_table, torch.int32, "page_table", dev), n, p, pages, h, d)
 
     @classmethod
     def empty(cls, n_pages, kv_heads, page_size, head_dim, page_table):
@@ -629,19 +657,6 @@ class KVCache:
                 for _ in range(2))
         ks, vs = (torch.ones(n_pages, kv_heads, dtype=torch.int32, device=dev) for _ in range(2))
         return cls(k, v, ks, vs, page_table)
-
-
-def _same_device(*tensors):
-    """Calls go to the current device's stream: every tensor has to be there."""
-    cur = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in tensors:
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != cur:
-            raise IlwError(f"a tensor on {t.device}, with cuda:{cur} the current device")
-
-
-def _shape(t, shape, name):
-    if tuple(t.shape) != tuple(shape):
-        raise IlwError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
 
 
 def rope_table(rows, rotary_dim, base=10000.0, device="cuda"):
@@ -659,31 +674,30 @@ def ilw_cache_append(cache: KVCache, qkv, heads, cu_new, past, max_new, rope=Non
     cu_new int32 [seqs + 1], past int32 [seqs], rope int16 [rows, rotary / 2, 2]
     or None (no rotation) -> q int8 [T, heads, head_dim], q_scale int32 [T,
     heads]; keys and values go to the cache."""
-    c = cache.struct
-    T = qkv.shape[0]
-    if qkv.dim() != 2 or qkv.shape[1] != (heads + 2 * c.kv_heads) * c.head_dim:
-        raise IlwError(f"qkv must be [tokens, {(heads + 2 * c.kv_heads) * c.head_dim}], got "
+    dev, D = _device(cache.k, "the cache"), cache.head_dim
+    if qkv.dim() != 2 or qkv.shape[1] != (heads + 2 * cache.kv_heads) * D:
+        raise IlwError(f"qkv must be [tokens, {(heads + 2 * cache.kv_heads) * D}], got "
                        f"{tuple(qkv.shape)}")
-    if not qkv.is_cuda or qkv.dtype != torch.int8 or (T > 0 and qkv.stride(1) != 1):
-        raise IlwError("qkv must be an int8 device tensor with contiguous rows")
+    T = qkv.shape[0]
+    if qkv.get_device() != dev or qkv.dtype is not torch.int8 or (T > 0 and qkv.stride(1) != 1):
+        raise IlwError(f"qkv must be an int8 tensor on cuda:{dev} with contiguous rows")
     _shape(cu_new, (cache.seqs + 1,), "cu_new")
     _shape(past, (cache.seqs,), "past")
     if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2):
         raise IlwError("rope must be [rows, rotary_dim / 2, 2]")
     if q is None:
-        q = torch.empty((T, heads, c.head_dim), dtype=torch.int8, device=qkv.device)
+        q = torch.empty((T, heads, D), dtype=torch.int8, device=qkv.device)
     if q_scale is None:
         q_scale = torch.empty((T, heads), dtype=torch.int32, device=qkv.device)
-    _shape(q, (T, heads, c.head_dim), "q")
+    _shape(q, (T, heads, D), "q")
     _shape(q_scale, (T, heads), "q_scale")
-    _same_device(cache.k, qkv, cu_new, past, rope, q, q_scale)
+    rows, pairs = (0, 0) if rope is None else rope.shape[:2]
     rc = lib().ilw_cache_append(
-        ctypes.byref(c), c_vp(qkv.data_ptr()), qkv.stride(0) if T > 1 else qkv.shape[1],
-        _dev(cu_new, torch.int32, "cu_new"), _dev(past, torch.int32, "past"),
-        None if rope is None else _dev(rope, torch.int16, "rope"),
-        0 if rope is None else rope.shape[0], 0 if rope is None else 2 * rope.shape[1],
-        int(interleaved), _dev(q, torch.int8, "q"), _dev(q_scale, torch.int32, "q_scale"), T,
-        cache.seqs, max_new, heads, _stream())
+        cache.struct, qkv.data_ptr(), qkv.stride(0) if T > 1 else qkv.shape[1],
+        _at(cu_new, torch.int32, "cu_new", dev), _at(past, torch.int32, "past", dev),
+        None if rope is None else _at(rope, torch.int16, "rope", dev), rows, 2 * pairs,
+        int(interleaved), _at(q, torch.int8, "q", dev), _at(q_scale, torch.int32, "q_scale", dev),
+        T, cache.seqs, max_new, heads, torch.cuda.current_stream(dev).cuda_stream)
     _check(rc, "ilw_cache_append")
     return q, q_scale
 
@@ -693,32 +707,32 @@ def ilw_cache_attention(cache: KVCache, q, q_scale, cu_q, lens, params: dict, ma
     """q int8 [T, heads, head_dim] and q_scale int32 [T, heads] over the cache's
     first lens[s] tokens of each sequence -> int8 [T, heads * head_dim].  params:
     score_mult, score_shift, out_mult, out_shift."""
-    c = cache.struct
-    if q.dim() != 3 or q.shape[2] != c.head_dim:
-        raise IlwError(f"q must be [tokens, heads, {c.head_dim}], got {tuple(q.shape)}")
-    T, heads, D = q.shape
+    dev, D = _device(cache.k, "the cache"), cache.head_dim
+    if q.dim() != 3 or q.shape[2] != D:
+        raise IlwError(f"q must be [tokens, heads, {D}], got {tuple(q.shape)}")
+    T, heads, _ = q.shape
     _shape(q_scale, (T, heads), "q_scale")
     _shape(cu_q, (cache.seqs + 1,), "cu_q")
     _shape(lens, (cache.seqs,), "lens")
     if out is None:
         out = torch.empty((T, heads * D), dtype=torch.int8, device=q.device)
-    if out.numel() != T * heads * D:
+    elif out.numel() != T * heads * D:
         raise IlwError(f"out must have {T * heads * D} elements, got {out.numel()}")
+    L = lib()
     if workspace is None:
-        need = lib().ilw_cache_attention_workspace_bytes(ctypes.byref(c), cache.seqs, max_q,
-                                                         max_len, heads)
+        need = L.ilw_cache_attention_workspace_bytes(cache.struct, cache.seqs, max_q, max_len,
+                                                     heads)
         if need == 0 and last_error():
             raise IlwError(f"ilw_cache_attention_workspace_bytes: {last_error()}")
-        workspace = torch.empty(max(need, 16), dtype=torch.int8, device=q.device)
-    _same_device(cache.k, q, q_scale, cu_q, lens, out, workspace)
-    ap = CacheAttnParams(int(params["score_mult"]), int(params["score_shift"]),
-                         int(params["out_mult"]), int(params["out_shift"]), int(causal),
-                         int(window))
-    rc = lib().ilw_cache_attention(
-        ctypes.byref(c), _dev(q, torch.int8, "q"), _dev(q_scale, torch.int32, "q_scale"),
-        _dev(cu_q, torch.int32, "cu_q"), _dev(lens, torch.int32, "lens"),
-        _dev(out, torch.int8, "out"), T, cache.seqs, max_q, max_len, heads, ctypes.byref(ap),
-        _dev(workspace, torch.int8, "workspace"), workspace.numel(), _stream())
+        workspace = torch.empty(need, dtype=torch.int8, device=q.device) if need else None
+    ap = CacheAttnParams(params["score_mult"], params["score_shift"], params["out_mult"],
+                         params["out_shift"], causal, window)
+    rc = L.ilw_cache_attention(
+        cache.struct, _at(q, torch.int8, "q", dev), _at(q_scale, torch.int32, "q_scale", dev),
+        _at(cu_q, torch.int32, "cu_q", dev), _at(lens, torch.int32, "lens", dev),
+        _at(out, torch.int8, "out", dev), T, cache.seqs, max_q, max_len, heads, ap,
+        None if workspace is None else _at(workspace, torch.int8, "workspace", dev),
+        0 if workspace is None else workspace.numel(), torch.cuda.current_stream(dev).cuda_stream)
     _check(rc, "ilw_cache_attention")
     return out
 
@@ -727,10 +741,11 @@ def ilw_linear_grouped(x, w, offsets, b, mult, shift, rows=None, y=None):
     """x int8 [R, K], w int8 [E, N, K], offsets int32 [E + 1], b int32 [E, N] or
     None, mult and shift int32 [1] or [E, N], rows int32 [M] (row of x for each
     row of y) or None (M = R) -> int8 [M, N]."""
+    dev = _device(x, "x")
     E, N, K = w.shape
     if x.dim() != 2 or x.shape[1] != K:
         raise IlwError(f"x must be [rows, {K}], got {tuple(x.shape)}")
-    M = x.shape[0] if rows is None else rows.shape[0]
+    M = x.shape[0] if rows is None else rows.numel()
     _shape(offsets, (E + 1,), "offsets")
     if b is not None:
         _shape(b, (E, N), "b")
@@ -739,13 +754,14 @@ def ilw_linear_grouped(x, w, offsets, b, mult, shift, rows=None, y=None):
     if y is None:
         y = torch.empty((M, N), dtype=torch.int8, device=x.device)
     _shape(y, (M, N), "y")
-    _same_device(x, w, offsets, b, mult, shift, rows, y)
     rc = lib().ilw_linear_grouped(
-        _dev(x, torch.int8, "x"), x.shape[0],
-        None if rows is None else _dev(rows, torch.int32, "rows"),
-        _dev(offsets, torch.int32, "offsets"), _dev(w, torch.int8, "w"),
-        None if b is None else _dev(b, torch.int32, "b"), _dyadic(mult, shift),
-        _dev(y, torch.int8, "y"), M, E, N, K, _stream())
+        _at(x, torch.int8, "x", dev), x.shape[0],
+        None if rows is None else _at(rows, torch.int32, "rows", dev),
+        _at(offsets, torch.int32, "offsets", dev), _at(w, torch.int8, "w", dev),
+        None if b is None else _at(b, torch.int32, "b", dev),
+        Dyadic(_at(mult, torch.int32, "mult", dev), _at(shift, torch.int32, "shift", dev),
+               mult.numel()),
+        _at(y, torch.int8, "y", dev), M, E, N, K, torch.cuda.current_stream(dev).cuda_stream)
     _check(rc, "ilw_linear_grouped")
     return y
 
