@@ -519,7 +519,8 @@ typedef struct {
 } ilw_cache_attn_params;
 
 size_t ilw_cache_attention_workspace_bytes(const ilw_kv_cache* cache, int32_t seqs,
-                                           int32_t max_q, int32_t max_len, int32_t heads);
+                                           int32_t max_q, int32_t max_len, int32_t heads,
+                                           int32_t window);
 int ilw_cache_attention(const ilw_kv_cache* cache, const int8_t* q, const int32_t* q_scale,
                         const int32_t* cu_q, const int32_t* lens, int8_t* out,
                         int32_t tokens, int32_t seqs, int32_t max_q, int32_t max_len,

@@ -40,7 +40,7 @@ FLAGS = ["-O3", f"--offload-arch={ARCH}", "-std=c++17", "-fPIC", "-Wall",
 # tokens of 4 x 192 channels to 256: 18.9 -> 13.9 us; 3072 tokens to 384: 10.1
 # -> 9.2 us); the GEMM tiles measured the same either way.
 SOURCE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-                for src in ("attention.hip", "split_conv.hip")}
+                for src in ("attention.hip", "split_conv.hip", "cache_attention.hip")}
 
 
 def build(verbose: bool = False) -> str:

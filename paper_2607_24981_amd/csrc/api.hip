@@ -1436,10 +1436,16 @@ int ilw_decoder_layer(const ilw_decoder_params* p, const int8_t* tgt, const int8
 }
 
 size_t ilw_cache_attention_workspace_bytes(const ilw_kv_cache* cache, int32_t seqs,
-                                           int32_t max_q, int32_t max_len, int32_t heads) {
+                                           int32_t max_q, int32_t max_len, int32_t heads,
+                                           int32_t window) {
   CacheAttnArgs a = {};
   if (check_cache(cache, seqs, &a.c) || check_cache_attention(a.c, seqs, max_q, max_len, heads))
     return 0;
+  if (window < 0) {
+    fail(ILW_E_PARAM, "window = %d must be >= 0", window);
+    return 0;
+  }
+  a.window = window < (1 << 21) ? window : 1 << 21;
   a.seqs = seqs;
   a.max_q = max_q;
   a.max_len = max_len;
@@ -1540,7 +1546,7 @@ int ilw_cache_attention(const ilw_kv_cache* cache, const int8_t* q, const int32_
   a.out_mult = ap->out_mult;
   a.out_shift = ap->out_shift;
   a.causal = ap->causal;
-  a.window = ap->window;
+  a.window = ap->window < (1 << 21) ? ap->window : 1 << 21;  // past every key
   const size_t need = cache_attention_workspace(a);
   REQUIRE(need == 0 || (workspace && workspace_bytes >= need), ILW_E_WORKSPACE,
           "workspace of %zu bytes needed, %zu given", need, workspace_bytes);

@@ -47,37 +47,104 @@ struct Span {
 };
 
 // The pages of 64 consecutive keys from key kb (a multiple of 64) on: one page,
-// or two or four.  GB: 16-key blocks of a page among them.  numbers() then
-// scales(): the second loads what the first one names.
+// or two or four.  GB: 16-key blocks of a page among them.  Keys of a page that is
+// not there are read from page 0; a negative key scale marks them.
 template <int GB>
 struct Pages {
   static constexpr int N = 4 / GB;
   int32_t page[N], ks[N], vs[N];
-  bool ok;  // every page is there
-  __device__ __forceinline__ void numbers(const CacheView& c, const int32_t* table, int32_t kb) {
+  __device__ __forceinline__ bool all() const {
+    int32_t m = ks[0];
 #pragma unroll
-    for (int i = 0; i < N; ++i) page[i] = table[min((kb >> c.lp) + i, c.max_pages - 1)];
-  }
-  // Keys of a page that is not there are read from page 0, and marked by a
-  // negative key scale.
-  __device__ __forceinline__ void scales(const CacheView& c, int32_t h) {
-    ok = true;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const bool there = (uint32_t)page[i] < (uint32_t)c.n_pages;
-      page[i] = there ? page[i] : 0;
-      const int64_t at = (int64_t)page[i] * c.Hkv + h;
-      ks[i] = there ? c.k_scale[at] : -1;
-      vs[i] = c.v_scale[at];
-      ok = ok && there;
-    }
+    for (int i = 1; i < N; ++i) m = min(m, ks[i]);
+    return m >= 0;
   }
   // byte offset of slot 0 of 16-key block u's page and head, and the block's slot
   __device__ __forceinline__ int64_t base(const CacheView& c, int32_t h, int u) const {
     return (((int64_t)page[u / GB] * c.Hkv + h) << c.lp) * c.D;
   }
+  // the same for a block number that is not a constant (selects, not an array in
+  // memory)
+  __device__ __forceinline__ int64_t base_at(const CacheView& c, int32_t h, int u) const {
+    int32_t p = page[0];
+#pragma unroll
+    for (int n = 1; n < N; ++n) p = u / GB == n ? page[n] : p;
+    return (((int64_t)p * c.Hkv + h) << c.lp) * c.D;
+  }
   __device__ __forceinline__ static int32_t slot(const CacheView& c, int32_t kb, int u) {
     return GB == 4 ? (kb & ((1 << c.lp) - 1)) + 16 * u : 16 * (u % GB);
+  }
+};
+
+// A sequence's page numbers and scales, 64 pages at a time, one a lane.  The next
+// 64 are loaded when the ones before them come into use, and the numbers of those
+// after them, so that nothing waits for the two loads in a row that a page takes
+// (as scalar loads, which share their counter with LDS reads, they held up every
+// step for their latency).
+template <int GB>
+struct PageList {
+  const int32_t* table;
+  int32_t first;                       // page of lane 0
+  int32_t page, ks, vs, page1, ks1, vs1, page2;
+  __device__ __forceinline__ int32_t number(const CacheView& c, int32_t at, int lane) const {
+    const int32_t p = table[min(at + lane, c.max_pages - 1)];
+    return (uint32_t)p < (uint32_t)c.n_pages ? p : -1;
+  }
+  __device__ __forceinline__ static void scales(const CacheView& c, int32_t h, int32_t p,
+                                                int32_t& k, int32_t& v) {
+    const int64_t at = (int64_t)max(p, 0) * c.Hkv + h;
+    k = c.k_scale[at];
+    v = c.v_scale[at];
+    k = p < 0 ? -1 : k;
+  }
+  __device__ __forceinline__ void numbers(const CacheView& c, const int32_t* t, int32_t kb, int lane) {
+    table = t;
+    first = kb >> c.lp;
+    page = number(c, first, lane);
+    page1 = number(c, first + 64, lane);
+    page2 = number(c, first + 128, lane);
+  }
+  __device__ __forceinline__ void init(const CacheView& c, const int32_t* t, int32_t h, int32_t kb,
+                                       int lane) {
+    numbers(c, t, kb, lane);
+    scales(c, h, page, ks, vs);
+    scales(c, h, page1, ks1, vs1);
+  }
+  // init after numbers(kb0) with kb0 <= kb
+  __device__ __forceinline__ void start(const CacheView& c, int32_t h, int32_t kb, int lane) {
+    if ((kb >> c.lp) - first >= 64) numbers(c, table, kb, lane);
+    scales(c, h, page, ks, vs);
+    scales(c, h, page1, ks1, vs1);
+  }
+  // The pages at kb, which is not before the last one asked for and less than 64
+  // pages past it, without their scales: those are scale()'s, to be asked for
+  // before the next pages are, but after the loads from these have been issued.
+  __device__ __forceinline__ Pages<GB> at(const CacheView& c, int32_t h, int32_t kb, int lane) {
+    if ((kb >> c.lp) - first >= 64) {
+      first += 64;
+      page = page1;
+      ks = ks1;
+      vs = vs1;
+      page1 = page2;
+      scales(c, h, page1, ks1, vs1);
+      page2 = number(c, first + 128, lane);
+    }
+    Pages<GB> r;
+    const int32_t i = (kb >> c.lp) - first;
+#pragma unroll
+    for (int n = 0; n < Pages<GB>::N; ++n) {
+      r.page[n] = max(__builtin_amdgcn_readlane(page, i + n), 0);
+      r.ks[n] = r.vs[n] = 0;
+    }
+    return r;
+  }
+  __device__ __forceinline__ void scale(const CacheView& c, int32_t kb, Pages<GB>& r) const {
+    const int32_t i = (kb >> c.lp) - first;
+#pragma unroll
+    for (int n = 0; n < Pages<GB>::N; ++n) {
+      r.ks[n] = __builtin_amdgcn_readlane(ks, i + n);
+      r.vs[n] = __builtin_amdgcn_readlane(vs, i + n);
+    }
   }
 };
 
@@ -129,7 +196,10 @@ __device__ __forceinline__ int32_t rescale(int32_t acc, int32_t m, int64_t c) {
 }
 // The multiplier of a row's products with the keys of a page.
 __device__ __forceinline__ int32_t score_mult(int32_t A, int32_t ks) {
-  return (int32_t)(((int64_t)A * ks + (1 << 15)) >> 16);
+  // (the low word by a byte permute of both: from a 64-bit shift the compiler
+  // would make the products below 64 x 64 bits wide)
+  const int64_t p = (int64_t)A * ks + (1 << 15);
+  return (int32_t)__builtin_amdgcn_perm((uint32_t)(p >> 32), (uint32_t)p, 0x05040302u);
 }
 
 constexpr int64_t kRnd = (int64_t)1 << 27;
@@ -248,11 +318,98 @@ __device__ __forceinline__ int32_t over_lanes(int32_t m) {  // of a row
   return max(m, __shfl_xor(m, 32, 64));
 }
 
-// Many rows: 16 NF rows of a (sequence, kv head) over all their keys twice, by one
-// wave.
+// ---- many rows: a wave takes 16 NF rows of a (sequence, kv head) over all their
+// keys twice.  The four waves of a workgroup share the keys and values of a step
+// (64 keys) in LDS, where they come straight from memory, two steps side by side:
+// the loads of a step are in flight during the products of the one before.
+__device__ __forceinline__ void load_lds16(const int8_t* src, int8_t* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
+// 64 keys in LDS: keys [head_dim / 64][64][64 bytes], their 16-byte chunks
+// swizzled as lds_chunk<4> has them (32-byte rows as they are), then the values as
+// they lie in memory, page after page.
+template <int D, int GB>
+struct Step {
+  static constexpr int CH = D >= 64 ? 4 : 2, BYTES = 64 * D;
+  // byte of this lane's page base among the step's (uniform where it can be)
+  template <int PER>
+  __device__ static __forceinline__ int64_t page_base(const CacheView& c, const Pages<GB>& pg,
+                                                      int32_t h, int q, int at) {
+    // PER chunks a page: instruction q covers chunks 64 q .. 64 q + 63
+    if constexpr (PER >= 64) {
+      return pg.base_at(c, h, (q * 64 / PER) * GB);
+    } else {
+      static_assert(PER == 32, "half an instruction a page");
+      const int64_t lo = pg.base_at(c, h, 2 * q * GB), hi = pg.base_at(c, h, (2 * q + 1) * GB);
+      return at < 32 ? lo : hi;
+    }
+  }
+  __device__ static __forceinline__ void keys(const CacheView& c, const Pages<GB>& pg, int32_t h,
+                                              int32_t kb, int8_t* lds, int wave, int lane) {
+#pragma unroll
+    for (int q = 0; q < (D / 16 + 3) / 4; ++q) {
+      const int i = q * 4 + wave;  // chunks 64 i .. 64 i + 63 of [kc][64][CH]
+      if (D < 64 && i >= D / 16) break;
+      const int kc = i / CH, part = i % CH;  // 64 / CH rows of it
+      const int row = part * (64 / CH) + lane / CH, ch = lane % CH;
+      const int sw = CH == 4 ? ch ^ ((row & 4) >> 1) : ch;
+      int64_t at;
+      if constexpr (CH == 4) {
+        at = pg.base_at(c, h, part) + (Pages<GB>::slot(c, kb, part) + (lane >> 2)) * D;
+      } else if constexpr (GB == 1) {
+        at = lane < 32 ? pg.base_at(c, h, 2 * part) : pg.base_at(c, h, 2 * part + 1);
+        at += (row & 15) * D;
+      } else {
+        at = pg.base_at(c, h, 2 * part) + (Pages<GB>::slot(c, kb, 2 * part) + (lane >> 1)) * D;
+      }
+      load_lds16(c.k + at + kc * 64 + sw * 16, lds + i * 1024);
+    }
+  }
+  __device__ static __forceinline__ void values(const CacheView& c, const Pages<GB>& pg, int32_t h,
+                                                int32_t kb, int8_t* lds, int wave, int lane) {
+    constexpr int PER = D * GB;  // 16-byte chunks a page
+    const int32_t s0 = GB == 4 ? Pages<GB>::slot(c, kb, 0) * D : 0;
+#pragma unroll
+    for (int q = 0; q < (D / 16 + 3) / 4; ++q) {
+      const int i = q * 4 + wave;
+      if (D < 64 && i >= D / 16) break;
+      load_lds16(c.v + page_base<PER>(c, pg, h, i, lane) + s0 + (i * 64 + lane) % PER * 16,
+                 lds + i * 1024);
+    }
+  }
+  __device__ static __forceinline__ v4i key(const int8_t* lds, int u, int kc, int lane) {
+    const int r = u * 16 + (lane & 15), c = lane >> 4;
+    if constexpr (CH == 4) return *(const v4i*)(lds + kc * 4096 + lds_chunk<4>(r, c));
+    else return lane < 32 ? *(const v4i*)(lds + r * 32 + c * 16) : v4i{0, 0, 0, 0};
+  }
+  __device__ static __forceinline__ v4i value(const int8_t* lds, int g, int lane) {
+    v4i v;
+    if constexpr (GB == 4) {
+      v = *(const v4i*)(lds + g * 1024 + lane * 16);
+    } else if constexpr (GB == 2) {
+      typedef int v2i __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const v2i x = *(const v2i*)(lds + i * (D * 32) + g * 512 + lane * 8);
+        v[2 * i] = x[0];
+        v[2 * i + 1] = x[1];
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = *(const int32_t*)(lds + u * (D * 16) + g * 256 + lane * 4);
+    }
+    return v;
+  }
+};
+
 template <int D, int GB, int NF>
-__global__ __launch_bounds__(256) void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
-  constexpr int CG = D / 16;
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
+  constexpr int CG = D / 16, KC = Keys<D>::KC;
+  typedef Step<D, GB> St;
+  __shared__ __attribute__((aligned(1024))) int8_t buf0[2 * St::BYTES], buf1[2 * St::BYTES];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t pair = blockIdx.x / tiles, tile = tiles - 1 - (blockIdx.x - pair * tiles);
@@ -260,60 +417,96 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(CacheAttnArgs a, uint32
   const int32_t G = a.Hq / a.c.Hkv;
   const int32_t* table = a.c.table + (int64_t)s * a.c.max_pages;
   const Seq sq(a, s);
-  const int32_t rows = sq.nq * G, r0 = ((int32_t)tile * 4 + wave) * 16 * NF;
-  if (r0 >= rows) return;
+  const int32_t rows = sq.nq * G, w0 = (int32_t)tile * 64 * NF;
+  if (w0 >= rows) return;
+  // waves past the last row repeat it; their results are not stored
+  const int32_t r0 = w0 + wave * 16 * NF;
   Rows<D, NF> R;
-  R.load(a, sq, h, G, r0, rows, lane);
-  const int32_t kb0 = R.any_lo & ~63, kend = R.any_hi;
+  R.load(a, sq, h, G, min(r0, rows - 1), rows, lane);
+  const Span s0(a, sq, w0 / G), s1(a, sq, (min(w0 + 64 * NF, rows) - 1) / G);
+  const int32_t kb0 = s0.lo & ~63, kend = s1.hi;
   auto full = [&](int32_t kb) { return kb >= R.all_lo && kb + 64 <= R.all_hi; };
+  auto none = [&](int32_t kb) { return kb + 64 <= R.any_lo || kb >= R.any_hi; };
   const v4i zero = {0, 0, 0, 0};
+  // body(buffer, kb, pages) for every step; each step's tile is complete, and the
+  // other buffer free, at the barrier ahead of it
+  auto steps = [&](auto with_values, auto body) {
+    constexpr bool V = decltype(with_values)::value;
+    PageList<GB> list;
+    list.init(a.c, table, h, kb0, lane);
+    Pages<GB> p0 = list.at(a.c, h, kb0, lane);
+    auto load = [&](const Pages<GB>& pg, int32_t kb, int8_t* buf) {
+      St::keys(a.c, pg, h, kb, buf, wave, lane);
+      if (V) St::values(a.c, pg, h, kb, buf + St::BYTES, wave, lane);
+    };
+    auto step = [&](int32_t kb, Pages<GB> pg, int8_t* buf, int8_t* other) {
+      __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt 0
+      lds_sync();
+      list.scale(a.c, kb, pg);
+      const Pages<GB> next = list.at(a.c, h, kb + 64, lane);
+      if (kb + 64 < kend) load(next, kb + 64, other);
+      if (!none(kb)) body(buf, kb, pg);
+      return next;
+    };
+    lds_sync();  // (the last user of the buffers is done)
+    if (kb0 < kend) load(p0, kb0, buf0);
+    for (int32_t kb = kb0; kb < kend; kb += 128) {
+      const Pages<GB> p1 = step(kb, p0, buf0, buf1);
+      if (kb + 64 >= kend) break;
+      p0 = step(kb + 64, p1, buf1, buf0);
+    }
+  };
+  auto products = [&](const int8_t* buf, int u, v4i(&p)[NF]) {
+#pragma unroll
+    for (int f = 0; f < NF; ++f) p[f] = zero;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) {
+      const v4i k = St::key(buf, u, kc, lane);
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+        p[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k, R.q[f][kc], p[f], 0, 0, 0);
+    }
+  };
 
-  // ---- maxima.  The keys of the next step, and the page numbers of the one
-  // after it, are on their way during a step (past the last one too: any page
-  // number leads to a page).
+  // ---- maxima
   int32_t M[NF];
 #pragma unroll
   for (int f = 0; f < NF; ++f) M[f] = kNone;
-  {
-    Pages<GB> p0, p1;
-    Keys<D> k0;
-    p0.numbers(a.c, table, kb0);
-    p1.numbers(a.c, table, kb0 + 64);
-    p0.scales(a.c, h);
-    k0.load(a.c, p0, h, kb0, lane);
-    for (int32_t kb = kb0; kb < kend; kb += 64) {
-      Pages<GB> p2;
-      Keys<D> k1;
-      p2.numbers(a.c, table, kb + 128);
-      p1.scales(a.c, h);
-      k1.load(a.c, p1, h, kb + 64, lane);
-      if (full(kb) && p0.ok) {
+  steps(Flag<false>{}, [&](const int8_t* buf, int32_t kb, const Pages<GB>& pg) {
+    if (full(kb) && pg.all()) {
+      v4i top[NF];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < 4; ++u) {
+        v4i p[NF];
+        products(buf, u, p);
+        // (products of one scale are compared before they are rescaled)
 #pragma unroll
-          for (int f = 0; f < NF; ++f) {
-            const v4i p = R.products(k0, u, f);
-            M[f] = max(max(M[f], -32767), rescale(max(max(p[0], p[1]), max(p[2], p[3])),
-                                                  score_mult(R.A[f], p0.ks[u / GB]), kRnd));
-          }
-      } else {
+        for (int f = 0; f < NF; ++f) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int f = 0; f < NF; ++f) {
-            const v4i p = R.products(k0, u, f);
-            const int32_t m = score_mult(R.A[f], p0.ks[u / GB]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (R.sees(f, kb + 16 * u + 4 * (lane >> 4) + r, p0.ks[u / GB]))
-                M[f] = max(max(M[f], -32767), rescale(p[r], m, kRnd));
-          }
+          for (int r = 0; r < 4; ++r) top[f][r] = u % GB == 0 ? p[f][r] : max(top[f][r], p[f][r]);
+          if (u % GB == GB - 1)
+            M[f] = max(max(M[f], -32767),
+                       rescale(max(max(top[f][0], top[f][1]), max(top[f][2], top[f][3])),
+                               score_mult(R.A[f], pg.ks[u / GB]), kRnd));
+        }
       }
-      p0 = p1;
-      p1 = p2;
-      k0 = k1;
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        v4i p[NF];
+        products(buf, u, p);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          const int32_t m = score_mult(R.A[f], pg.ks[u / GB]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int32_t x = max(rescale(p[f][r], m, kRnd), -32767);
+            M[f] = max(M[f], R.sees(f, kb + 16 * u + 4 * (lane >> 4) + r, pg.ks[u / GB]) ? x : kNone);
+          }
+        }
+      }
     }
-  }
+  });
   Ref ref[NF];
 #pragma unroll
   for (int f = 0; f < NF; ++f) ref[f].init(over_lanes(M[f]));
@@ -327,61 +520,43 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(CacheAttnArgs a, uint32
 #pragma unroll
     for (int g = 0; g < CG; ++g) oh[g][f] = ol[g][f] = zero;
   }
-  {
-    Pages<GB> p0, p1;
-    Keys<D> k0;
-    p0.numbers(a.c, table, kb0);
-    p1.numbers(a.c, table, kb0 + 64);
-    p0.scales(a.c, h);
-    k0.load(a.c, p0, h, kb0, lane);
-    for (int32_t kb = kb0; kb < kend; kb += 64) {
-      Pages<GB> p2;
-      p2.numbers(a.c, table, kb + 128);
-      p1.scales(a.c, h);
-      v4i vf[CG];
+  steps(Flag<true>{}, [&](const int8_t* buf, int32_t kb, const Pages<GB>& pg) {
+    v4i ph[NF], pl[NF];
+    auto weights = [&](auto checked) {
 #pragma unroll
-      for (int g = 0; g < CG; ++g) vf[g] = load_values<D, GB>(a.c, p0, h, kb, g, lane);
-      v4i sc[4][NF];
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int f = 0; f < NF; ++f) sc[u][f] = R.products(k0, u, f);
-      k0.load(a.c, p1, h, kb + 64, lane);
-      const bool fast = full(kb) && p0.ok;
-      v4i ph[NF], pl[NF];
-      auto weights = [&](auto checked) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int f = 0; f < NF; ++f) {
-            const int32_t m = score_mult(R.A[f], p0.ks[u / GB]);
-            uint32_t w[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              w[r] = weight(med3(rescale(sc[u][f][r], m, ref[f].c), ref[f].cap, 0));
-              if (decltype(checked)::value &&
-                  !R.sees(f, kb + 16 * u + 4 * (lane >> 4) + r, p0.ks[u / GB]))
-                w[r] = 0;
-            }
-            L[f] += w[0] + w[1] + w[2] + w[3];
-            const Digits d(w, (uint32_t)p0.vs[u / GB]);
-            ph[f][u] = (int)d.hi;
-            pl[f][u] = (int)d.lo;
-          }
-      };
-      if (fast) weights(Flag<false>{});
-      else weights(Flag<true>{});
-#pragma unroll
-      for (int g = 0; g < CG; ++g)
+      for (int u = 0; u < 4; ++u) {
+        v4i p[NF];
+        products(buf, u, p);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
-          oh[g][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[g], ph[f], oh[g][f], 0, 0, 0);
-          ol[g][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[g], pl[f], ol[g][f], 0, 0, 0);
+          const int32_t m = score_mult(R.A[f], pg.ks[u / GB]);
+          uint32_t w[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            w[r] = weight(med3(rescale(p[f][r], m, ref[f].c), ref[f].cap, 0));
+            if (decltype(checked)::value &&
+                !R.sees(f, kb + 16 * u + 4 * (lane >> 4) + r, pg.ks[u / GB]))
+              w[r] = 0;
+          }
+          L[f] += w[0] + w[1] + w[2] + w[3];
+          const Digits d(w, (uint32_t)pg.vs[u / GB]);
+          ph[f][u] = (int)d.hi;
+          pl[f][u] = (int)d.lo;
         }
-      p0 = p1;
-      p1 = p2;
+      }
+    };
+    if (full(kb) && pg.all()) weights(Flag<false>{});
+    else weights(Flag<true>{});
+#pragma unroll
+    for (int g = 0; g < CG; ++g) {
+      const v4i v = St::value(buf + St::BYTES, g, lane);
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        oh[g][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v, ph[f], oh[g][f], 0, 0, 0);
+        ol[g][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v, pl[f], ol[g][f], 0, 0, 0);
+      }
     }
-  }
+  });
 #pragma unroll
   for (int f = 0; f < NF; ++f) {
     Norm nm;
@@ -407,12 +582,13 @@ struct Split {
   int32_t* top;     // [tiles][nsplit][16]
   int64_t* T;       // [tiles][nsplit][rpt][D]
   uint64_t* L;      // [tiles][nsplit][16]
-  int32_t rt, rpt, steps, nsplit, chunk;  // row tiles a pair, rows a tile, keys a split
+  int32_t tiles, rt, rpt, steps, nsplit, chunk;  // tiles a pair, rows a tile, keys a part
 };
 
-// The tile of a workgroup: its sequence, kv head and rows, and its chunks of keys.
+// The tile of a workgroup: its sequence, kv head and rows, and the keys that some
+// of them see, end - base of them from a multiple of 64 on, in `parts` parts.
 struct Few {
-  int32_t s, h, G, r0, rows, first, last;  // chunks first .. last - 1 hold keys
+  int32_t s, h, G, r0, rows, base, end, parts;
   __device__ __forceinline__ Few(const CacheAttnArgs& a, const Split& sp, uint32_t tile) {
     const uint32_t pair = tile / (uint32_t)sp.rt;
     s = (int32_t)(pair / (uint32_t)a.c.Hkv);
@@ -424,8 +600,9 @@ struct Few {
     rows = sq.nq * G;
     if (r0 >= rows) return false;
     const Span s0(a, sq, r0 / G), s1(a, sq, (min(r0 + 16, rows) - 1) / G);
-    first = s0.lo / sp.chunk;
-    last = s1.hi > s0.lo ? (s1.hi + sp.chunk - 1) / sp.chunk : first;
+    base = s0.lo & ~63;
+    end = s1.hi;
+    parts = end > s0.lo ? (end - base + sp.chunk - 1) / sp.chunk : 0;
     return true;
   }
 };
@@ -434,24 +611,22 @@ struct Few {
 // out(step, words); the row's maximum over them comes back.
 template <int D, int GB, int NW, typename Out>
 __device__ __forceinline__ int32_t few_scores(const CacheAttnArgs& a, const Rows<D, 1>& R,
-                                              const int32_t* table, int32_t h, int32_t c0,
+                                              PageList<GB> list, int32_t h, int32_t c0,
                                               int32_t c1, int wave, int lane, Out out) {
   int32_t M = kNone;
   const int32_t kb0 = c0 + wave * 64;
   if (kb0 >= c1) return M;
-  Pages<GB> p0, p1;
+  list.start(a.c, h, kb0, lane);
+  Pages<GB> p0 = list.at(a.c, h, kb0, lane);
   Keys<D> k0;
-  p0.numbers(a.c, table, kb0);
-  p1.numbers(a.c, table, kb0 + 64 * NW);
-  p0.scales(a.c, h);
   k0.load(a.c, p0, h, kb0, lane);
   for (int32_t kb = kb0; kb < c1; kb += 64 * NW) {
-    Pages<GB> p2;
+    list.scale(a.c, kb, p0);
+    // (past the last step too: any page number leads to a page)
+    const Pages<GB> p1 = list.at(a.c, h, kb + 64 * NW, lane);
     Keys<D> k1;
-    p2.numbers(a.c, table, kb + 128 * NW);
-    p1.scales(a.c, h);
     k1.load(a.c, p1, h, kb + 64 * NW, lane);
-    const bool fast = kb >= R.all_lo && kb + 64 <= R.all_hi && p0.ok;
+    const bool fast = kb >= R.all_lo && kb + 64 <= R.all_hi && p0.all();
     v4i w[2];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -471,38 +646,41 @@ __device__ __forceinline__ int32_t few_scores(const CacheAttnArgs& a, const Rows
     }
     out(kb >> 6, w);
     p0 = p1;
-    p1 = p2;
     k0 = k1;
   }
   return M;
 }
 
-// Weights and sums of the same steps, the scores from in(step).
-template <int D, int GB, int NW, typename In>
-__device__ __forceinline__ uint32_t few_values(const CacheAttnArgs& a, const Ref& ref,
-                                               const int32_t* table, int32_t h, int32_t c0,
-                                               int32_t c1, int wave, int lane, In in,
-                                               v4i (&oh)[D / 16], v4i (&ol)[D / 16]) {
+// Weights and sums of the same steps, the scores from in(step); the reference
+// from top(), which may wait for the other waves, once the first values are on
+// their way.
+template <int D, int GB, int NW, typename Top, typename In>
+__device__ __forceinline__ uint32_t few_values(const CacheAttnArgs& a, PageList<GB> list, int32_t h,
+                                               int32_t c0, int32_t c1, int wave, int lane, Top top,
+                                               In in, v4i (&oh)[D / 16], v4i (&ol)[D / 16]) {
   constexpr int CG = D / 16;
   uint32_t L = 0;
   const v4i zero = {0, 0, 0, 0};
 #pragma unroll
   for (int g = 0; g < CG; ++g) oh[g] = ol[g] = zero;
   const int32_t kb0 = c0 + wave * 64;
-  if (kb0 >= c1) return L;
-  Pages<GB> p0, p1;
+  Pages<GB> p0;
   v4i v0[CG];
-  p0.numbers(a.c, table, kb0);
-  p1.numbers(a.c, table, kb0 + 64 * NW);
-  p0.scales(a.c, h);
+  if (kb0 < c1) {
+    list.start(a.c, h, kb0, lane);
+    p0 = list.at(a.c, h, kb0, lane);
 #pragma unroll
-  for (int g = 0; g < CG; ++g) v0[g] = load_values<D, GB>(a.c, p0, h, kb0, g, lane);
+    for (int g = 0; g < CG; ++g) v0[g] = load_values<D, GB>(a.c, p0, h, kb0, g, lane);
+  }
+  // (a wave's own scores: no other wave's are read)
+  v4i x0[2];
+  if (kb0 < c1) in(kb0 >> 6, x0);
+  const Ref ref = top();
   for (int32_t kb = kb0; kb < c1; kb += 64 * NW) {
-    Pages<GB> p2;
-    v4i v1[CG], x[2], ph, pl;
-    in(kb >> 6, x);
-    p2.numbers(a.c, table, kb + 128 * NW);
-    p1.scales(a.c, h);
+    v4i v1[CG], x1[2], ph, pl;
+    if (kb + 64 * NW < c1) in((kb >> 6) + NW, x1);
+    list.scale(a.c, kb, p0);
+    const Pages<GB> p1 = list.at(a.c, h, kb + 64 * NW, lane);
 #pragma unroll
     for (int g = 0; g < CG; ++g) v1[g] = load_values<D, GB>(a.c, p1, h, kb + 64 * NW, g, lane);
 #pragma unroll
@@ -510,7 +688,7 @@ __device__ __forceinline__ uint32_t few_values(const CacheAttnArgs& a, const Ref
       uint32_t w[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int32_t two = x[u / 2][(u % 2) * 2 + r / 2];
+        const int32_t two = x0[u / 2][(u % 2) * 2 + r / 2];
         const int32_t sc = r % 2 ? two >> 16 : (int16_t)two;
         w[r] = sc == kNone ? 0 : weight(med3(sc - ref.m, ref.cap, 0));
       }
@@ -525,7 +703,8 @@ __device__ __forceinline__ uint32_t few_values(const CacheAttnArgs& a, const Ref
       ol[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v0[g], pl, ol[g], 0, 0, 0);
     }
     p0 = p1;
-    p1 = p2;
+    x0[0] = x1[0];
+    x0[1] = x1[1];
 #pragma unroll
     for (int g = 0; g < CG; ++g) v0[g] = v1[g];
   }
@@ -556,6 +735,24 @@ struct FewSums {
       }
   }
   __device__ __forceinline__ int64_t T(int i) const { return (int64_t)hi[i] * 256 + lo[i]; }
+
+  // A tile's output.
+  template <typename Few>
+  __device__ __forceinline__ void write(const CacheAttnArgs& a, const Few& t, int32_t first,
+                                        int32_t rows) const {
+    for (int i = threadIdx.x; i < D / 16 * 64; i += 64 * NW) {
+      const int ln = i & 63, g = i >> 6, row = ln & 15;
+      if (row >= rows) continue;
+      Norm nm;
+      nm.init(L[row]);
+      int32_t v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = nm.out(T(i * 4 + k), a.out_mult, a.out_shift);
+      const int32_t r = t.r0 + row, q = r / t.G;
+      *(uint32_t*)(a.out + ((int64_t)(first + q) * a.Hq + t.h * t.G + r - q * t.G) * D + g * 16 +
+                   (ln >> 4) * 4) = pack4(v[0], v[1], v[2], v[3]);
+    }
+  }
 };
 
 // One workgroup for all keys of a tile.
@@ -567,73 +764,72 @@ __global__ __launch_bounds__(64 * NW) void cache_few_kernel(CacheAttnArgs a, Spl
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Few t(a, sp, blockIdx.x);
-  const int32_t* table = a.c.table + (int64_t)t.s * a.c.max_pages;
+  PageList<GB> list;
+  list.numbers(a.c, a.c.table + (int64_t)t.s * a.c.max_pages, wave * 64, lane);
   const Seq sq(a, t.s);
   if (!t.bounds(a, sp, sq)) return;
   Rows<D, 1> R;
   R.load(a, sq, t.h, t.G, t.r0, t.rows, lane);
-  const int32_t n = min(16, t.rows - t.r0), c0 = R.any_lo & ~63;
+  const int32_t n = min(16, t.rows - t.r0);
   int16_t* scores = (int16_t*)dyn + (lane >> 4) * 16 + (lane & 15) * 64;
-  const int32_t stride = sp.rpt * 64, s0 = c0 >> 6;
+  const int32_t stride = sp.rpt * 64, s0 = t.base >> 6;
   sums.clear();
   const int32_t M = over_lanes(few_scores<D, GB, NW>(
-      a, R, table, t.h, c0, R.any_hi, wave, lane, [&](int32_t step, const v4i(&w)[2]) {
+      a, R, list, t.h, t.base, t.end, wave, lane, [&](int32_t step, const v4i(&w)[2]) {
         if ((lane & 15) >= n) return;
         v4i* p = (v4i*)(scores + (step - s0) * stride);
         p[0] = w[0];
         p[1] = w[1];
       }));
   if (lane < 16) top[wave][lane] = M;
-  lds_sync();
-  int32_t m = kNone;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) m = max(m, top[w][lane & 15]);
-  Ref ref;
-  ref.init(m);
   v4i oh[D / 16], ol[D / 16];
   const int32_t back = max((lane & 15) - (n - 1), 0) * 64;  // rows past the last repeat it
   const uint32_t L = few_values<D, GB, NW>(
-      a, ref, table, t.h, c0, R.any_hi, wave, lane, [&](int32_t step, v4i(&x)[2]) {
+      a, list, t.h, t.base, t.end, wave, lane,
+      [&] {
+        lds_sync();
+        int32_t m = kNone;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m = max(m, top[w][lane & 15]);
+        Ref ref;
+        ref.init(m);
+        return ref;
+      },
+      [&](int32_t step, v4i(&x)[2]) {
         const v4i* p = (const v4i*)(scores + (step - s0) * stride - back);
         x[0] = p[0];
         x[1] = p[1];
       }, oh, ol);
   sums.add(L, oh, ol, n, lane);
   lds_sync();
-  for (int i = threadIdx.x; i < D / 16 * 64; i += 64 * NW) {
-    const int ln = i & 63, g = i >> 6, row = ln & 15;
-    if (row >= n) continue;
-    Norm nm;
-    nm.init(sums.L[row]);
-    int32_t v[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = nm.out(sums.T(i * 4 + k), a.out_mult, a.out_shift);
-    const int32_t r = t.r0 + row, q = r / t.G;
-    *(uint32_t*)(a.out + ((int64_t)(sq.first + q) * a.Hq + t.h * t.G + r - q * t.G) * D + g * 16 +
-                 (ln >> 4) * 4) = pack4(v[0], v[1], v[2], v[3]);
-  }
+  sums.write(a, t, sq.first, n);
 }
 
-// Several workgroups a tile, three launches: scores and maxima, sums, the output.
+// Several workgroups a tile, in launches of their own: scores and maxima, sums,
+// and, where a tile has several parts, the output.
 template <int D, int GB>
 __global__ __launch_bounds__(256) void split_scores_kernel(CacheAttnArgs a, Split sp) {
   __shared__ int32_t top[4][16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t tile = blockIdx.x / (uint32_t)sp.nsplit;
-  const int32_t part = (int32_t)(blockIdx.x - tile * (uint32_t)sp.nsplit);
+  // (a part's tiles side by side: later parts are shorter or empty, and with a
+  // tile's parts side by side some XCDs had only those: the sums of 32
+  // sequences of 2048 to 8192 keys 45.0 us so, 42.7 now)
+  const uint32_t part_u = blockIdx.x / (uint32_t)sp.tiles, tile = blockIdx.x - part_u * (uint32_t)sp.tiles;
+  const int32_t part = (int32_t)part_u;
   Few t(a, sp, tile);
-  const int32_t* table = a.c.table + (int64_t)t.s * a.c.max_pages;
+  PageList<GB> list;
+  list.numbers(a.c, a.c.table + (int64_t)t.s * a.c.max_pages, part * sp.chunk + wave * 64, lane);
   const Seq sq(a, t.s);
-  if (!t.bounds(a, sp, sq) || part < t.first || part >= t.last) return;
+  if (!t.bounds(a, sp, sq) || part >= t.parts) return;
   Rows<D, 1> R;
   R.load(a, sq, t.h, t.G, t.r0, t.rows, lane);
   const int32_t n = min(16, t.rows - t.r0);
-  const int32_t c0 = max(part * sp.chunk, R.any_lo & ~63), c1 = min((part + 1) * sp.chunk, R.any_hi);
-  int16_t* scores = sp.scores + (int64_t)tile * sp.steps * sp.rpt * 64 + (lane >> 4) * 16 +
-                    (lane & 15) * 64;
+  const int32_t c0 = t.base + part * sp.chunk, c1 = min(c0 + sp.chunk, t.end);
+  int16_t* scores = sp.scores + ((int64_t)tile * sp.steps - (t.base >> 6)) * sp.rpt * 64 +
+                    (lane >> 4) * 16 + (lane & 15) * 64;
   const int32_t M = over_lanes(few_scores<D, GB, 4>(
-      a, R, table, t.h, c0, c1, wave, lane, [&](int32_t step, const v4i(&w)[2]) {
+      a, R, list, t.h, c0, c1, wave, lane, [&](int32_t step, const v4i(&w)[2]) {
         if ((lane & 15) >= n) return;
         v4i* p = (v4i*)(scores + (int64_t)step * sp.rpt * 64);
         p[0] = w[0];
@@ -652,35 +848,56 @@ __global__ __launch_bounds__(256) void split_scores_kernel(CacheAttnArgs a, Spli
 template <int D, int GB>
 __global__ __launch_bounds__(256) void split_values_kernel(CacheAttnArgs a, Split sp) {
   __shared__ __attribute__((aligned(16))) FewSums<D, 4> sums;
+  __shared__ int32_t top[4][16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t tile = blockIdx.x / (uint32_t)sp.nsplit;
-  const int32_t part = (int32_t)(blockIdx.x - tile * (uint32_t)sp.nsplit);
+  // (a part's tiles side by side: later parts are shorter or empty, and with a
+  // tile's parts side by side some XCDs had only those: the sums of 32
+  // sequences of 2048 to 8192 keys 45.0 us so, 42.7 now)
+  const uint32_t part_u = blockIdx.x / (uint32_t)sp.tiles, tile = blockIdx.x - part_u * (uint32_t)sp.tiles;
+  const int32_t part = (int32_t)part_u;
   Few t(a, sp, tile);
-  const int32_t* table = a.c.table + (int64_t)t.s * a.c.max_pages;
+  PageList<GB> list;
+  list.numbers(a.c, a.c.table + (int64_t)t.s * a.c.max_pages, part * sp.chunk + wave * 64, lane);
   const Seq sq(a, t.s);
-  if (!t.bounds(a, sp, sq) || part < t.first || part >= t.last) return;
-  const Span s0(a, sq, t.r0 / t.G), s1(a, sq, (min(t.r0 + 16, t.rows) - 1) / t.G);
+  if (!t.bounds(a, sp, sq)) return;
   const int32_t n = min(16, t.rows - t.r0);
-  const int32_t c0 = max(part * sp.chunk, s0.lo & ~63), c1 = min((part + 1) * sp.chunk, s1.hi);
+  // (without a join the only part writes the output, zeros where no key is seen)
+  if (part >= t.parts && sp.nsplit > 1) return;
+  const int32_t c0 = t.base + part * sp.chunk, c1 = min(c0 + sp.chunk, t.end);
   sums.clear();
-  int32_t m = kNone;
-  for (int32_t i = t.first + (lane >> 4); i < t.last; i += 4)
-    m = max(m, sp.top[((int64_t)tile * sp.nsplit + i) * 16 + (lane & 15)]);
-  Ref ref;
-  ref.init(over_lanes(m));
-  const int16_t* scores = sp.scores + (int64_t)tile * sp.steps * sp.rpt * 64 + (lane >> 4) * 16 +
-                          min(lane & 15, n - 1) * 64;
+  const int16_t* scores = sp.scores + ((int64_t)tile * sp.steps - (t.base >> 6)) * sp.rpt * 64 +
+                          (lane >> 4) * 16 + min(lane & 15, n - 1) * 64;
   v4i oh[D / 16], ol[D / 16];
   const uint32_t L = few_values<D, GB, 4>(
-      a, ref, table, t.h, c0, c1, wave, lane, [&](int32_t step, v4i(&x)[2]) {
+      a, list, t.h, c0, c1, wave, lane,
+      [&] {
+        // the parts' maxima, 16 side by side
+        const int32_t* all = sp.top + (int64_t)tile * sp.nsplit * 16 + (lane & 15);
+        int32_t m = kNone;
+#pragma unroll 4
+        for (int32_t i = wave * 4 + (lane >> 4); i < t.parts; i += 16)
+          m = max(m, all[i * 16]);
+        m = over_lanes(m);
+        if (lane < 16) top[wave][lane] = m;
+        lds_sync();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = max(m, top[w][lane & 15]);
+        Ref ref;
+        ref.init(m);
+        return ref;
+      },
+      [&](int32_t step, v4i(&x)[2]) {
         const v4i* p = (const v4i*)(scores + (int64_t)step * sp.rpt * 64);
         x[0] = p[0];
         x[1] = p[1];
       }, oh, ol);
-  lds_sync();
   sums.add(L, oh, ol, n, lane);
   lds_sync();
+  if (sp.nsplit == 1) {
+    sums.write(a, t, sq.first, n);
+    return;
+  }
   const int64_t at = (int64_t)tile * sp.nsplit + part;
   for (int i = threadIdx.x; i < D / 16 * 64; i += 256) {
     const int ln = i & 63, g = i >> 6, row = ln & 15;
@@ -707,7 +924,7 @@ __global__ __launch_bounds__(256) void split_join_kernel(CacheAttnArgs a, Split 
   int64_t T[4] = {0, 0, 0, 0};
   uint64_t L = 0;
 #pragma unroll 4
-  for (int32_t i = t.first + p0; i < t.last; i += PP) {
+  for (int32_t i = p0; i < t.parts; i += PP) {
     const int64_t at = (int64_t)tile * sp.nsplit + i;
     const int64_t* src = sp.T + (at * sp.rpt + row) * D + q * 4;
 #pragma unroll
@@ -750,33 +967,44 @@ Plan plan(const CacheAttnArgs& a) {
   const int64_t G = a.Hq / a.c.Hkv, rows = a.max_q * G, pairs = (int64_t)a.seqs * a.c.Hkv;
   p.sp.rt = (int32_t)((rows + 15) / 16);
   p.sp.rpt = (int32_t)(rows < 16 ? rows : 16);
-  p.sp.steps = (a.max_len + 63) / 64;
+  // keys that a tile's rows (at most 16 queries) can see
+  const int64_t seen = a.window && (int64_t)a.window + 16 < a.max_len ? a.window + 16 : a.max_len;
+  p.sp.steps = (int32_t)((seen + 63) / 64) + (seen < a.max_len);
   p.tiles = pairs * p.sp.rt;
+  p.sp.tiles = (int32_t)p.tiles;
   p.sp.nsplit = 1;
   p.sp.chunk = p.sp.steps * 64 + 64;
   if (p.tiles == 0 || p.sp.steps == 0) {
     p.way = FEW;
     return p;
   }
-  if (rows > 64 && a.max_len <= 131072) {
+  // Many rows, and enough of them to fill the CUs: the kernel that shares keys
+  // among the rows of a workgroup (128, or 64 of 256 channels).  16 heads of 600
+  // queries over 4696 keys each are 80 workgroups: 110 us so, 64 us split.
+  const int64_t shared = pairs * ((rows + (a.c.D >= 256 ? 63 : 127)) / (a.c.D >= 256 ? 64 : 128));
+  if (rows > 64 && shared >= 192 && a.max_len <= 131072) {
     p.way = ROWS;
     return p;
   }
   const size_t lds = (size_t)p.sp.steps * p.sp.rpt * 128;
-  if (a.max_len <= 1024 && lds <= 32768) {
+  if (seen <= 1024 && lds <= 32768) {
     p.way = FEW;
     return p;
   }
   p.way = SPLIT;
-  int64_t chunk = (a.max_len * p.tiles + 1023) / 1024;
+  // Parts enough for two workgroups a CU, of at least 512 keys.  (131072 keys of 8
+  // kv heads in 512, 1024 and 2048 parts: 30, 32 and 36 us for the scores, 29, 34
+  // and 42 for the sums: a part costs its start.)
+  int64_t chunk = (seen * p.tiles + 511) / 512;
   chunk = (chunk + 255) / 256 * 256;
   if (chunk < 512) chunk = 512;
   if (chunk > 32768) chunk = 32768;
   p.sp.chunk = (int32_t)chunk;
-  p.sp.nsplit = (int32_t)((a.max_len + chunk - 1) / chunk);
+  p.sp.nsplit = (int32_t)((p.sp.steps * 64 + chunk - 1) / chunk);
   const int64_t parts = p.tiles * p.sp.nsplit;
-  p.bytes = align256((size_t)p.tiles * p.sp.steps * p.sp.rpt * 128) + align256((size_t)parts * 64) +
-            align256((size_t)parts * p.sp.rpt * a.c.D * 8) + align256((size_t)parts * 128);
+  p.bytes = align256((size_t)p.tiles * p.sp.steps * p.sp.rpt * 128) + align256((size_t)parts * 64);
+  if (p.sp.nsplit > 1)
+    p.bytes += align256((size_t)parts * p.sp.rpt * a.c.D * 8) + align256((size_t)parts * 128);
   return p;
 }
 
@@ -817,7 +1045,7 @@ hipError_t launch_pages(const CacheAttnArgs& a, void* ws, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((split_values_kernel<D, GB>), dim3((unsigned)parts), dim3(256), 0, s, a, p.sp);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if ((e = hipGetLastError()) != hipSuccess || p.sp.nsplit == 1) return e;
   hipLaunchKernelGGL((split_join_kernel<D>), dim3((unsigned)(p.tiles * p.sp.rpt)), dim3(256), 0, s, a,
                      p.sp);
   return hipGetLastError();

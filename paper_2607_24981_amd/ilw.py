@@ -128,7 +128,7 @@ _SIGS = {
                                         c_vp, c_i32, c_i32, c_i32, c_vp, c_vp] + [c_i32] * 4 +
                          [c_vp]),
     "ilw_cache_attention_workspace_bytes": (c_size, [ctypes.POINTER(KVCacheStruct)] +
-                                            [c_i32] * 4),
+                                            [c_i32] * 5),
     "ilw_cache_attention": (ctypes.c_int, [ctypes.POINTER(KVCacheStruct)] + [c_vp] * 5 +
                             [c_i32] * 5 + [ctypes.POINTER(CacheAttnParams), c_vp, c_size, c_vp]),
     "ilw_linear_grouped": (ctypes.c_int, [c_vp, c_i64, c_vp, c_vp, c_vp, c_vp, Dyadic, c_vp,
@@ -721,7 +721,7 @@ def ilw_cache_attention(cache: KVCache, q, q_scale, cu_q, lens, params: dict, ma
     L = lib()
     if workspace is None:
         need = L.ilw_cache_attention_workspace_bytes(cache.struct, cache.seqs, max_q, max_len,
-                                                     heads)
+                                                     heads, window)
         if need == 0 and last_error():
             raise IlwError(f"ilw_cache_attention_workspace_bytes: {last_error()}")
         workspace = torch.empty(need, dtype=torch.int8, device=q.device) if need else None

@@ -57,7 +57,7 @@ def test_cache_refusals(kw, code):
     c = cache(**kw)
     assert append(c, seqs=3, ld=4096, rope_rows=1 << 21, rotary=0) == code
     assert attention(c, seqs=3, max_len=0) == code
-    assert ilw.lib().ilw_cache_attention_workspace_bytes(ctypes.byref(c), 3, 1, 0, 4) == 0
+    assert ilw.lib().ilw_cache_attention_workspace_bytes(ctypes.byref(c), 3, 1, 0, 4, 0) == 0
     assert ilw.last_error()
 
 
@@ -97,6 +97,23 @@ def attention(c=None, ap=None, **kw):
 def test_attention_refusals(kw, code):
     assert attention(**kw) == code
     assert bool(ilw.last_error()) == (code != OK)
+
+
+def test_attention_workspace():
+    """Grows with the keys that can be seen, and the call wants as much."""
+    def need(max_q, max_len, window, seqs=8):
+        return ilw.lib().ilw_cache_attention_workspace_bytes(
+            ctypes.byref(cache(max_pages=2048)), seqs, max_q, max_len, 4, window)
+    assert need(1, 500, 0) == 0 and need(1, 0, 0) == 0 and need(0, 5000, 0) == 0
+    assert 0 < need(1, 20000, 0) < need(1, 100000, 0)
+    assert need(1, 100000, 4096) < need(1, 100000, 0)
+    assert need(1, 100000, 2 ** 31 - 1) == need(1, 100000, 0)
+    assert need(1, 100000, -1) == 0 and ilw.last_error()
+    big = cache(max_pages=2048)
+    n = need(1, 20000, 0)
+    for ws, size in [(None, n), (FAKE, n - 1)]:
+        assert attention(big, seqs=8, max_q=1, max_len=20000, workspace=ws, size=size) == E_WS
+    assert attention(big, seqs=8, max_q=1, max_len=20000, workspace=FAKE + 8, size=n) == E_PARAM
 
 
 def test_attention_rows_limit():

@@ -196,6 +196,43 @@ def test_attention_rows(D, P, heads, hk, causal, window):
                   first=3, pad=5)
 
 
+@pytest.mark.parametrize("D,P,heads,hk", [(64, 64, 6, 2), (128, 16, 4, 1), (32, 32, 2, 2),
+                                          (256, 128, 3, 1), (128, 64, 16, 2), (64, 16, 5, 1)])
+@pytest.mark.parametrize("new,window", [(1, 0), (1, 1500), (11, 0), (9, 700)])
+def test_attention_long(D, P, heads, hk, new, window):
+    """Keys split over workgroups: lengths around the parts' borders, in one
+    call with short and empty ones; the parts of a window start anywhere."""
+    lens = [2600, 1, 511, 512, 513, 1025, 0, 2048, 1536]
+    g = rng(D, P, heads, new, window)
+    c = make_cache(g, len(lens), -(-2600 // P), hk, P, D)
+    c["table"][2, 3] = -1
+    counts = [new] * 4 + [max(1, new // 2)] * 5
+    run_attention(c, heads, counts, lens, params(D), True, window,
+                  f"long D={D} P={P} heads={heads}/{hk} new={new} window={window}", g=g)
+
+
+@pytest.mark.parametrize("D,P,heads,hk", [(64, 16, 8, 4), (128, 64, 6, 3), (32, 32, 4, 4),
+                                          (256, 128, 4, 4), (128, 16, 3, 3), (32, 16, 8, 4),
+                                          (256, 16, 4, 4), (64, 256, 5, 5), (128, 32, 4, 4)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 45)])
+def test_attention_many_rows(D, P, heads, hk, causal, window):
+    """Grids that fill the GPU with the rows of prompts: 192 tiles and more."""
+    seqs = 64 if hk > 3 else 80
+    g = rng(D, P, heads, causal, window)
+    new = [int(x) for x in g.integers(0, 12, seqs)]
+    lens = [n + int(x) for n, x in zip(new, g.integers(0, 60, seqs))]
+    G = heads // hk
+    new[3], lens[3] = 70 // G + 40, 70 // G + 41      # over one tile, the last partly filled
+    new[5], lens[5] = 90, 50                          # more queries than keys
+    new[7], lens[7] = 66, 0
+    new[9], lens[9] = 130 // G, 300
+    c = make_cache(g, seqs, -(-300 // P), hk, P, D)
+    c["table"][9, ::2] = -1
+    run_attention(c, heads, new, lens, params(D), causal, window,
+                  f"many rows D={D} P={P} heads={heads}/{hk} causal={causal} window={window}", g=g,
+                  first=2, pad=3)
+
+
 @pytest.mark.parametrize("octaves", [0.0, 0.02, 30.0, 500.0, 4000.0])
 def test_attention_score_ranges(octaves):
     """Flat rows, single peaks, scores past 16 bits; a scale that is refused."""
