@@ -194,6 +194,12 @@ __device__ __forceinline__ int32_t rescale(int32_t acc, int32_t m, int64_t c) {
   const int64_t p = (int64_t)acc * m + c;
   return (int32_t)__builtin_amdgcn_alignbit((uint32_t)(p >> 32), (uint32_t)p, 28);
 }
+// The same of m and c scaled by 2^4 (HI), where the host has shown that every
+// multiplier stays below 2^27: the high word as it is.
+template <bool HI>
+__device__ __forceinline__ int32_t rescale(int32_t acc, int32_t m, int64_t c) {
+  return HI ? (int32_t)(((int64_t)acc * m + c) >> 32) : rescale(acc, m, c);
+}
 // The multiplier of a row's products with the keys of a page.
 __device__ __forceinline__ int32_t score_mult(int32_t A, int32_t ks) {
   // (the low word by a byte permute of both: from a 64-bit shift the compiler
@@ -248,9 +254,12 @@ struct Norm {
     F = L ? div_2p31m1((uint32_t)(L >> d)) : 0;
     sh = d + 13;
   }
-  __device__ __forceinline__ int32_t out(int64_t T, int32_t mult, int32_t shift) const {
-    const int32_t r = (int32_t)((T * (int64_t)F) >> sh);
-    return rq(r, mult, shift);
+  // |r| < 2^25; past +-clamp the result saturates (clamp_bound on the host), within
+  // it the shifted product fits 32 bits
+  __device__ __forceinline__ int32_t out(int64_t T, const CacheAttnArgs& a) const {
+    const int32_t r = med3((int32_t)((T * (int64_t)F) >> sh), -a.out_clamp, a.out_clamp);
+    const int64_t v = (int64_t)r * a.out_mult + ((int64_t)1 << (a.out_shift - 1));
+    return med3((int32_t)(v >> a.out_shift), kQmin, kQmax);
   }
 };
 
@@ -404,12 +413,14 @@ struct Step {
   }
 };
 
-template <int D, int GB, int NF>
+// HI: rescale<true>.
+template <int D, int GB, int NF, bool HI>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
 void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
-  constexpr int CG = D / 16, KC = Keys<D>::KC;
+  constexpr int CG = D / 16, KC = Keys<D>::KC, UP = HI ? 4 : 0;
+  constexpr int64_t RND = kRnd << UP;
   typedef Step<D, GB> St;
-  __shared__ __attribute__((aligned(1024))) int8_t buf0[2 * St::BYTES], buf1[2 * St::BYTES];
+  __shared__ __attribute__((aligned(1024))) int8_t even[2 * St::BYTES], odd[2 * St::BYTES];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t pair = blockIdx.x / tiles, tile = tiles - 1 - (blockIdx.x - pair * tiles);
@@ -428,32 +439,32 @@ void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
   auto full = [&](int32_t kb) { return kb >= R.all_lo && kb + 64 <= R.all_hi; };
   auto none = [&](int32_t kb) { return kb + 64 <= R.any_lo || kb >= R.any_hi; };
   const v4i zero = {0, 0, 0, 0};
-  // body(buffer, kb, pages) for every step; each step's tile is complete, and the
-  // other buffer free, at the barrier ahead of it
+  // body(kb, pages, tile) for every step; its tile (keys, then values) is complete,
+  // and the other buffer free, at the barrier ahead of it
   auto steps = [&](auto with_values, auto body) {
     constexpr bool V = decltype(with_values)::value;
     PageList<GB> list;
     list.init(a.c, table, h, kb0, lane);
     Pages<GB> p0 = list.at(a.c, h, kb0, lane);
-    auto load = [&](const Pages<GB>& pg, int32_t kb, int8_t* buf) {
-      St::keys(a.c, pg, h, kb, buf, wave, lane);
-      if (V) St::values(a.c, pg, h, kb, buf + St::BYTES, wave, lane);
+    auto load = [&](const Pages<GB>& pg, int32_t kb, int8_t* to) {
+      St::keys(a.c, pg, h, kb, to, wave, lane);
+      if (V) St::values(a.c, pg, h, kb, to + St::BYTES, wave, lane);
     };
-    auto step = [&](int32_t kb, Pages<GB> pg, int8_t* buf, int8_t* other) {
+    auto step = [&](int32_t kb, Pages<GB> pg, int8_t* tile, int8_t* other) {
       __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt 0
       lds_sync();
       list.scale(a.c, kb, pg);
       const Pages<GB> next = list.at(a.c, h, kb + 64, lane);
       if (kb + 64 < kend) load(next, kb + 64, other);
-      if (!none(kb)) body(buf, kb, pg);
+      if (!none(kb)) body(kb, pg, tile);
       return next;
     };
     lds_sync();  // (the last user of the buffers is done)
-    if (kb0 < kend) load(p0, kb0, buf0);
+    if (kb0 < kend) load(p0, kb0, even);
     for (int32_t kb = kb0; kb < kend; kb += 128) {
-      const Pages<GB> p1 = step(kb, p0, buf0, buf1);
+      const Pages<GB> p1 = step(kb, p0, even, odd);
       if (kb + 64 >= kend) break;
-      p0 = step(kb + 64, p1, buf1, buf0);
+      p0 = step(kb + 64, p1, odd, even);
     }
   };
   auto products = [&](const int8_t* buf, int u, v4i(&p)[NF]) {
@@ -472,13 +483,13 @@ void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
   int32_t M[NF];
 #pragma unroll
   for (int f = 0; f < NF; ++f) M[f] = kNone;
-  steps(Flag<false>{}, [&](const int8_t* buf, int32_t kb, const Pages<GB>& pg) {
+  steps(Flag<false>{}, [&](int32_t kb, const Pages<GB>& pg, const int8_t* keys) {
     if (full(kb) && pg.all()) {
       v4i top[NF];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         v4i p[NF];
-        products(buf, u, p);
+        products(keys, u, p);
         // (products of one scale are compared before they are rescaled)
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
@@ -486,21 +497,21 @@ void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
           for (int r = 0; r < 4; ++r) top[f][r] = u % GB == 0 ? p[f][r] : max(top[f][r], p[f][r]);
           if (u % GB == GB - 1)
             M[f] = max(max(M[f], -32767),
-                       rescale(max(max(top[f][0], top[f][1]), max(top[f][2], top[f][3])),
-                               score_mult(R.A[f], pg.ks[u / GB]), kRnd));
+                       rescale<HI>(max(max(top[f][0], top[f][1]), max(top[f][2], top[f][3])),
+                                   score_mult(R.A[f], pg.ks[u / GB]) << UP, RND));
         }
       }
     } else {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         v4i p[NF];
-        products(buf, u, p);
+        products(keys, u, p);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
-          const int32_t m = score_mult(R.A[f], pg.ks[u / GB]);
+          const int32_t m = score_mult(R.A[f], pg.ks[u / GB]) << UP;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int32_t x = max(rescale(p[f][r], m, kRnd), -32767);
+            const int32_t x = max(rescale<HI>(p[f][r], m, RND), -32767);
             M[f] = max(M[f], R.sees(f, kb + 16 * u + 4 * (lane >> 4) + r, pg.ks[u / GB]) ? x : kNone);
           }
         }
@@ -509,7 +520,10 @@ void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
   });
   Ref ref[NF];
 #pragma unroll
-  for (int f = 0; f < NF; ++f) ref[f].init(over_lanes(M[f]));
+  for (int f = 0; f < NF; ++f) {
+    ref[f].init(over_lanes(M[f]));
+    ref[f].c = ref[f].c * (1 << UP);
+  }
 
   // ---- weights and sums
   v4i oh[CG][NF], ol[CG][NF];
@@ -520,20 +534,20 @@ void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
 #pragma unroll
     for (int g = 0; g < CG; ++g) oh[g][f] = ol[g][f] = zero;
   }
-  steps(Flag<true>{}, [&](const int8_t* buf, int32_t kb, const Pages<GB>& pg) {
+  steps(Flag<true>{}, [&](int32_t kb, const Pages<GB>& pg, const int8_t* keys) {
     v4i ph[NF], pl[NF];
     auto weights = [&](auto checked) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         v4i p[NF];
-        products(buf, u, p);
+        products(keys, u, p);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
-          const int32_t m = score_mult(R.A[f], pg.ks[u / GB]);
+          const int32_t m = score_mult(R.A[f], pg.ks[u / GB]) << UP;
           uint32_t w[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            w[r] = weight(med3(rescale(p[f][r], m, ref[f].c), ref[f].cap, 0));
+            w[r] = weight(med3(rescale<HI>(p[f][r], m, ref[f].c), ref[f].cap, 0));
             if (decltype(checked)::value &&
                 !R.sees(f, kb + 16 * u + 4 * (lane >> 4) + r, pg.ks[u / GB]))
               w[r] = 0;
@@ -549,7 +563,7 @@ void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
     else weights(Flag<true>{});
 #pragma unroll
     for (int g = 0; g < CG; ++g) {
-      const v4i v = St::value(buf + St::BYTES, g, lane);
+      const v4i v = St::value(keys + St::BYTES, g, lane);
 #pragma unroll
       for (int f = 0; f < NF; ++f) {
         oh[g][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v, ph[f], oh[g][f], 0, 0, 0);
@@ -567,7 +581,7 @@ void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
       int32_t v[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        v[r] = nm.out((int64_t)oh[g][f][r] * 256 + ol[g][f][r], a.out_mult, a.out_shift);
+        v[r] = nm.out((int64_t)oh[g][f][r] * 256 + ol[g][f][r], a);
       *(uint32_t*)(a.out + R.at[f] * D + g * 16 + (lane >> 4) * 4) = pack4(v[0], v[1], v[2], v[3]);
     }
   }
@@ -747,7 +761,7 @@ struct FewSums {
       nm.init(L[row]);
       int32_t v[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = nm.out(T(i * 4 + k), a.out_mult, a.out_shift);
+      for (int k = 0; k < 4; ++k) v[k] = nm.out(T(i * 4 + k), a);
       const int32_t r = t.r0 + row, q = r / t.G;
       *(uint32_t*)(a.out + ((int64_t)(first + q) * a.Hq + t.h * t.G + r - q * t.G) * D + g * 16 +
                    (ln >> 4) * 4) = pack4(v[0], v[1], v[2], v[3]);
@@ -945,7 +959,7 @@ __global__ __launch_bounds__(256) void split_join_kernel(CacheAttnArgs a, Split 
   for (int k = 0; k < 4; ++k) {
     int64_t x = 0;
     for (int i = 0; i < PP; ++i) x += part_T[i][q * 4 + k];
-    v[k] = nm.out(x, a.out_mult, a.out_shift);
+    v[k] = nm.out(x, a);
   }
   const int32_t r = t.r0 + row, i = r / t.G;
   *(uint32_t*)(a.out + ((int64_t)(sq.first + i) * a.Hq + t.h * t.G + r - i * t.G) * D + q * 4) =
@@ -1018,8 +1032,14 @@ hipError_t launch_pages(const CacheAttnArgs& a, void* ws, hipStream_t s) {
     const uint32_t tiles = (uint32_t)((rows + 64 * NF - 1) / (64 * NF));
     const int64_t total = (int64_t)tiles * a.seqs * a.c.Hkv;
     if (total >= ((int64_t)1 << 24)) return hipErrorInvalidValue;  // under 2^32 threads
-    hipLaunchKernelGGL((cache_rows_kernel<D, GB, NF>), dim3((unsigned)total), dim3(256), 0, s, a,
-                       tiles);
+    // the largest multiplier that scales within their bounds can make
+    const int64_t A = (33026 * (int64_t)a.score_mult + ((int64_t)1 << (a.score_t - 1))) >> a.score_t;
+    if ((A * 37154 + (1 << 15)) >> 16 < (1 << 27))
+      hipLaunchKernelGGL((cache_rows_kernel<D, GB, NF, true>), dim3((unsigned)total), dim3(256), 0, s,
+                         a, tiles);
+    else
+      hipLaunchKernelGGL((cache_rows_kernel<D, GB, NF, false>), dim3((unsigned)total), dim3(256), 0,
+                         s, a, tiles);
     return hipGetLastError();
   }
   if (p.tiles * p.sp.nsplit >= ((int64_t)1 << 23) || p.tiles * 16 >= ((int64_t)1 << 24))
@@ -1061,7 +1081,12 @@ hipError_t launch_dim(const CacheAttnArgs& a, void* ws, hipStream_t s) {
 
 size_t cache_attention_workspace(const CacheAttnArgs& a) { return plan(a).bytes; }
 
-hipError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, hipStream_t s) {
+hipError_t launch_cache_attention(const CacheAttnArgs& args, void* ws, hipStream_t s) {
+  CacheAttnArgs a = args;
+  // beyond |r| = L the output saturates: |r m| >= 129 2^s (r stays below 2^25)
+  const int64_t am = a.out_mult < 0 ? -(int64_t)a.out_mult : (int64_t)a.out_mult;
+  const int64_t L = am && a.out_shift <= 54 ? 129 * ((int64_t)1 << a.out_shift) / am + 1 : 1 << 30;
+  a.out_clamp = (int32_t)(L < (1 << 30) ? L : 1 << 30);
   switch (a.c.D) {
     case 32: return launch_dim<32>(a, ws, s);
     case 64: return launch_dim<64>(a, ws, s);

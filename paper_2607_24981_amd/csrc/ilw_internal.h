@@ -638,6 +638,7 @@ struct CacheAttnArgs {
   int8_t* out;
   int32_t T, seqs, max_q, max_len, Hq;
   int32_t score_mult, score_t, out_mult, out_shift, causal, window;
+  int32_t out_clamp;  // set by launch_cache_attention
 };
 size_t cache_attention_workspace(const CacheAttnArgs& a);
 hipError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, hipStream_t s);
