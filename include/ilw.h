@@ -473,7 +473,9 @@ typedef struct {
  * page_size or in pages that are not there, are not appended beyond those
  * limits; query rows are written for the first max_new tokens of each
  * sequence.  Rows outside every sequence are left as they are.  tokens and
- * seqs may be 0.  One launch; no workspace.
+ * seqs may be 0.  One launch; no workspace.  A launch holds 2^24 workgroups
+ * (each 256/(head_dim/16) groups of 8 query heads, or a page of a kv head's keys
+ * or values): more are refused with ILW_E_UNSUPPORTED.
  */
 int ilw_cache_append(const ilw_kv_cache* cache, const int8_t* qkv, int64_t ld,
                      const int32_t* cu_new, const int32_t* past, const int16_t* rope,
@@ -511,6 +513,11 @@ int ilw_cache_append(const ilw_kv_cache* cache, const int8_t* qkv, int64_t ld,
  * past max_len are not there.  max_len <= max_pages * page_size.
  * q_scale in [1, 33026], page scales in [1, 37154] (keys) and [1, 18577]
  * (values), which ilw_cache_append keeps to.  The workspace may hold anything.
+ * Its size is that of the call's seqs, max_q, max_len, heads and window; where
+ * few rows or more than 131072 keys are split over the machine it holds two
+ * bytes for each query row and key, so that a prompt longer than that is given
+ * in pieces.  Calls whose rows need more than a launch's 2^32 threads are
+ * refused with ILW_E_UNSUPPORTED.
  */
 typedef struct {
   int32_t score_mult, score_shift;
@@ -537,8 +544,9 @@ int ilw_cache_attention(const ilw_kv_cache* cache, const int8_t* q, const int32_
  *            outside [offsets[0], offsets[experts]) are left as they are
  *   w int8 [experts, N, K], b int32 [experts, N] or NULL, y int8 [M, N]
  *   rq       n = 1 (one factor for all) or experts * N
- * N and K multiples of 16, K <= 131072, experts in [1, 1024]; x and w 16-byte
- * aligned, y 4-byte aligned and not aliasing x.  M == 0 is a no-op.
+ * N and K multiples of 16, K <= 131072, experts in [1, 1024], (M/64 + experts) *
+ * (N/128 + 1) < 2^22 (whole quotients); x and w 16-byte aligned, y 4-byte
+ * aligned and not aliasing x.  M == 0 is a no-op.
  */
 int ilw_linear_grouped(const int8_t* x, int64_t x_rows, const int32_t* rows,
                        const int32_t* offsets, const int8_t* w, const int32_t* b,

@@ -1496,6 +1496,9 @@ int ilw_cache_append(const ilw_kv_cache* cache, const int8_t* qkv, int64_t ld,
   a.seqs = seqs;
   a.max_new = max_new < tokens ? max_new : tokens;
   a.Hq = heads;
+  REQUIRE(cache_append_fits(a), ILW_E_UNSUPPORTED,
+          "seqs = %d of max_new = %d tokens and %d + %d heads: too many for a launch", seqs,
+          a.max_new, heads, cache->kv_heads);
   hipStream_t s = (hipStream_t)stream;
   StageTimer t(ILW_STAGE_CACHE_APPEND, s);
   const hipError_t he = launch_cache_append(a, s);
@@ -1547,6 +1550,9 @@ int ilw_cache_attention(const ilw_kv_cache* cache, const int8_t* q, const int32_
   a.out_shift = ap->out_shift;
   a.causal = ap->causal;
   a.window = ap->window < (1 << 21) ? ap->window : 1 << 21;  // past every key
+  REQUIRE(cache_attention_fits(a), ILW_E_UNSUPPORTED,
+          "seqs = %d of max_q = %d queries, max_len = %d keys and %d heads: too many for a launch",
+          seqs, max_q, max_len, heads);
   const size_t need = cache_attention_workspace(a);
   REQUIRE(need == 0 || (workspace && workspace_bytes >= need), ILW_E_WORKSPACE,
           "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
@@ -1572,8 +1578,10 @@ int ilw_linear_grouped(const int8_t* x, int64_t x_rows, const int32_t* rows,
           "experts * N = %lld must be below 2^31", (long long)experts * N);
   REQUIRE(M < ((int64_t)1 << 31) && x_rows < ((int64_t)1 << 31), ILW_E_UNSUPPORTED,
           "M=%lld and x_rows=%lld must be below 2^31", (long long)M, (long long)x_rows);
-  REQUIRE((M / 16 + experts) * ((N + 63) / 64) < (int64_t)1 << 31, ILW_E_UNSUPPORTED,
-          "too many tiles");
+  // (the grid of every tile size then stays under 2^32 threads)
+  REQUIRE((M / 64 + experts) * (N / 128 + 1) < (int64_t)1 << 22, ILW_E_UNSUPPORTED,
+          "(M / 64 + experts) * (N / 128 + 1) = %lld must be below 2^22",
+          (long long)((M / 64 + experts) * (N / 128 + 1)));
   REQUIRE(rows || x_rows >= M, ILW_E_SHAPE, "x has %lld rows, %lld needed", (long long)x_rows,
           (long long)M);
   if (M == 0) return ok();

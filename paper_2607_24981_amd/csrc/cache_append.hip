@@ -323,24 +323,39 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a, uint32_t nb, u
 
 }  // namespace
 
+namespace {
+
+struct Grid {
+  bool few;
+  int32_t hpu;
+  int64_t nb, units, kv_blocks, q_blocks, total;
+  explicit Grid(const AppendArgs& a) {
+    const int32_t P = 1 << a.c.lp;
+    // pages that max_new tokens can reach, whatever slot the first one takes
+    nb = ((int64_t)a.max_new + P - 2) / P + 1;
+    if (nb > a.c.max_pages) nb = a.c.max_pages;
+    units = nb * a.seqs * 2 * a.c.Hkv;
+    few = a.max_new <= 8;
+    kv_blocks = few ? (units + 3) / 4 : units;
+    hpu = few ? 1 : 8;
+    const int32_t groups = (a.Hq + hpu - 1) / hpu, per = NT / (a.c.D / 16);
+    q_blocks = ((int64_t)a.max_new * groups + per - 1) / per;
+    total = kv_blocks + q_blocks * a.seqs;
+  }
+};
+
+}  // namespace
+
+bool cache_append_fits(const AppendArgs& a) { return Grid(a).total < ((int64_t)1 << 24); }
+
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
-  const int32_t P = 1 << a.c.lp;
-  // pages that max_new tokens can reach, whatever slot the first one takes
-  int64_t nb = ((int64_t)a.max_new + P - 2) / P + 1;
-  if (nb > a.c.max_pages) nb = a.c.max_pages;
-  const int64_t units = nb * a.seqs * 2 * a.c.Hkv;
-  const bool few = a.max_new <= 8;
-  const int64_t kv_blocks = few ? (units + 3) / 4 : units;
-  const int32_t hpu = few ? 1 : 8, groups = (a.Hq + hpu - 1) / hpu, per = NT / (a.c.D / 16);
-  const int64_t q_blocks = ((int64_t)a.max_new * groups + per - 1) / per;
-  const int64_t total = kv_blocks + q_blocks * a.seqs;
-  if (total >= ((int64_t)1 << 24)) return hipErrorInvalidValue;  // under 2^32 threads
+  const Grid g(a);
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)total), dim3(NT), 0, s, a, (uint32_t)nb,
-                       (uint32_t)units, (uint32_t)kv_blocks, hpu, (uint32_t)q_blocks);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)g.total), dim3(NT), 0, s, a, (uint32_t)g.nb,
+                       (uint32_t)g.units, (uint32_t)g.kv_blocks, g.hpu, (uint32_t)g.q_blocks);
     return hipGetLastError();
   };
-  return few ? launch(append_kernel<64>) : launch(append_kernel<256>);
+  return g.few ? launch(append_kernel<64>) : launch(append_kernel<256>);
 }
 
 }  // namespace ilw

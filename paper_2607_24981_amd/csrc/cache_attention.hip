@@ -971,8 +971,9 @@ enum Way { ROWS, FEW, SPLIT };
 struct Plan {
   Way way;
   Split sp;
-  int64_t tiles;
-  size_t bytes;  // of the workspace
+  int64_t tiles;   // of 16 rows
+  int64_t rows, shared;  // of a kv head; workgroups of ROWS
+  size_t bytes;    // of the workspace
 };
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
@@ -995,8 +996,9 @@ Plan plan(const CacheAttnArgs& a) {
   // Many rows, and enough of them to fill the CUs: the kernel that shares keys
   // among the rows of a workgroup (128, or 64 of 256 channels).  16 heads of 600
   // queries over 4696 keys each are 80 workgroups: 110 us so, 64 us split.
-  const int64_t shared = pairs * ((rows + (a.c.D >= 256 ? 63 : 127)) / (a.c.D >= 256 ? 64 : 128));
-  if (rows > 64 && shared >= 192 && a.max_len <= 131072) {
+  p.rows = rows;
+  p.shared = pairs * ((rows + (a.c.D >= 256 ? 63 : 127)) / (a.c.D >= 256 ? 64 : 128));
+  if (rows > 64 && p.shared >= 192 && a.max_len <= 131072) {
     p.way = ROWS;
     return p;
   }
@@ -1028,10 +1030,8 @@ hipError_t launch_pages(const CacheAttnArgs& a, void* ws, hipStream_t s) {
   if (p.tiles == 0) return hipSuccess;
   if (p.way == ROWS) {
     constexpr int NF = D >= 256 ? 1 : 2;
-    const int64_t rows = (int64_t)a.max_q * (a.Hq / a.c.Hkv);
-    const uint32_t tiles = (uint32_t)((rows + 64 * NF - 1) / (64 * NF));
-    const int64_t total = (int64_t)tiles * a.seqs * a.c.Hkv;
-    if (total >= ((int64_t)1 << 24)) return hipErrorInvalidValue;  // under 2^32 threads
+    const uint32_t tiles = (uint32_t)((p.rows + 64 * NF - 1) / (64 * NF));
+    const int64_t total = p.shared;
     // the largest multiplier that scales within their bounds can make
     const int64_t A = (33026 * (int64_t)a.score_mult + ((int64_t)1 << (a.score_t - 1))) >> a.score_t;
     if ((A * 37154 + (1 << 15)) >> 16 < (1 << 27))
@@ -1042,8 +1042,6 @@ hipError_t launch_pages(const CacheAttnArgs& a, void* ws, hipStream_t s) {
                          s, a, tiles);
     return hipGetLastError();
   }
-  if (p.tiles * p.sp.nsplit >= ((int64_t)1 << 23) || p.tiles * 16 >= ((int64_t)1 << 24))
-    return hipErrorInvalidValue;
   if (p.way == FEW) {
     constexpr int NW = 8;
     hipLaunchKernelGGL((cache_few_kernel<D, GB, NW>), dim3((unsigned)p.tiles), dim3(64 * NW),
@@ -1080,6 +1078,13 @@ hipError_t launch_dim(const CacheAttnArgs& a, void* ws, hipStream_t s) {
 }  // namespace
 
 size_t cache_attention_workspace(const CacheAttnArgs& a) { return plan(a).bytes; }
+
+// (every grid below 2^32 threads)
+bool cache_attention_fits(const CacheAttnArgs& a) {
+  const Plan p = plan(a);
+  if (p.way == ROWS) return p.shared < ((int64_t)1 << 24);
+  return p.tiles * p.sp.nsplit < ((int64_t)1 << 23) && p.tiles * 16 < ((int64_t)1 << 24);
+}
 
 hipError_t launch_cache_attention(const CacheAttnArgs& args, void* ws, hipStream_t s) {
   CacheAttnArgs a = args;

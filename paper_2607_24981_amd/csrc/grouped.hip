@@ -8,13 +8,16 @@
 // by a wave-wide scan over the experts' tile counts and leaves if there is none.
 // A tile is WN x WM waves of FI x FJ MFMA tiles of 16 channels x 16 tokens.
 // Operands go from memory straight to LDS, 16 bytes a lane, in two buffers: the
-// loads of step k + 1 are in flight during the products of step k.
+// loads of step k + 1 are in flight during the products of step k.  (Weights read
+// straight to registers where few rows use them: 34 us against 22, since a load
+// then takes 64 bytes of 16 rows where these take whole 128-byte lines.)
 #include "ilw_internal.h"
 
 namespace ilw {
 namespace {
 
 constexpr int NXCD = 8;
+constexpr int KB = 128;  // inputs of a step: one cache line of each row
 
 __device__ __forceinline__ int32_t wave_scan_i32(int32_t v, int lane) {
 #pragma unroll
@@ -25,32 +28,51 @@ __device__ __forceinline__ int32_t wave_scan_i32(int32_t v, int lane) {
   return v;
 }
 
-// Expert and rows m0 .. m1 - 1 (at most TM) of a token tile; m0 == m1: none.
+// A workgroup's tile: expert e, rows m0 .. m1 - 1 (at most TM; m0 == m1: none),
+// channels from n0 on.
 struct Tile {
-  int32_t e, m0, m1;
+  int32_t e, m0, m1, n0;
 };
-template <int TM>
-__device__ __forceinline__ Tile find_tile(const GroupedArgs& a, int32_t tile, int lane) {
-  int32_t before = 0;
-  for (int32_t e0 = 0; e0 < a.E; e0 += 64) {
-    const int32_t e = e0 + lane;
-    int32_t lo = 0, hi = 0;
+// The tiles that hold rows are numbered expert by expert, the channel tiles of a
+// token tile next to each other, and each XCD takes one run of numbers: what
+// shares rows or weights shares an L2. The run is a share of the tiles there are,
+// not of the grid, whose last tiles are the ones that the offsets leave without rows.
+template <int TM, int TN>
+__device__ __forceinline__ Tile find_tile(const GroupedArgs& a, uint32_t tiles_n, int lane) {
+  const auto count = [&](int32_t e, int32_t& lo, int32_t& hi) {
+    lo = hi = 0;
     if (e < a.E) {
       lo = min(max(a.offsets[e], 0), (int32_t)a.M);
       hi = min(max(a.offsets[e + 1], lo), (int32_t)a.M);
     }
-    const int32_t n = (hi - lo + TM - 1) / TM, sum = before + wave_scan_i32(n, lane);
+    return (hi - lo + TM - 1) / TM;
+  };
+  int32_t lo, hi, n = count(lane, lo, hi), sum = wave_scan_i32(n, lane);
+  uint32_t live = __builtin_amdgcn_readlane(sum, 63);
+  for (int32_t e0 = 64; e0 < a.E; e0 += 64) {
+    int32_t l, h;
+    live += __builtin_amdgcn_readlane(wave_scan_i32(count(e0 + lane, l, h), lane), 63);
+  }
+  live *= tiles_n;
+  const uint32_t xcd = blockIdx.x % NXCD, i = blockIdx.x / NXCD, per = live / NXCD,
+                 rem = live % NXCD;
+  if (i >= per + (xcd < rem)) return {0, 0, 0, 0};
+  const uint32_t t = xcd * per + min(xcd, rem) + i, tm = t / tiles_n;
+  const int32_t tile = (int32_t)tm, n0 = (int32_t)(t - tm * tiles_n) * TN;
+  for (int32_t e0 = 0;;) {
     const uint64_t hit = __ballot(sum > tile);
     if (hit) {
       const int l = __ffsll((unsigned long long)hit) - 1;
-      const int32_t first = __shfl(sum - n, l, 64);
-      const int32_t m0 = __shfl(lo, l, 64) + (tile - first) * TM, m1 = __shfl(hi, l, 64);
-      return {__builtin_amdgcn_readfirstlane(e0 + l), __builtin_amdgcn_readfirstlane(m0),
-              __builtin_amdgcn_readfirstlane(min(m0 + TM, m1))};
+      const int32_t m0 = __builtin_amdgcn_readlane(lo, l) +
+                         (tile - __builtin_amdgcn_readlane(sum - n, l)) * TM;
+      return {e0 + l, m0, min(m0 + TM, __builtin_amdgcn_readlane(hi, l)), n0};
     }
-    before = __shfl(sum, 63, 64);
+    e0 += 64;
+    if (e0 >= a.E) return {0, 0, 0, 0};
+    const int32_t before = __builtin_amdgcn_readlane(sum, 63);
+    n = count(e0 + lane, lo, hi);
+    sum = before + wave_scan_i32(n, lane);
   }
-  return {0, 0, 0};
 }
 
 __device__ __forceinline__ void load_lds16(const int8_t* src, int8_t* dst) {
@@ -60,9 +82,8 @@ __device__ __forceinline__ void load_lds16(const int8_t* src, int8_t* dst) {
 
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt 0
 
-template <int WN, int WM, int FI, int FJ, int KB, bool KTAIL>
-__global__ __launch_bounds__(64 * WN * WM) void grouped_kernel(GroupedArgs a, uint32_t tiles_n,
-                                                              uint32_t tiles_total) {
+template <int WN, int WM, int FI, int FJ, bool KTAIL>
+__global__ __launch_bounds__(64 * WN * WM) void grouped_kernel(GroupedArgs a, uint32_t tiles_n) {
   constexpr int WTN = 16 * FI, WTM = 16 * FJ, TN = WTN * WN, TM = WTM * WM, NW = WN * WM,
                 NT = 64 * NW;
   constexpr int CPR = KB / 16, STAGE = (TN + TM) * KB;
@@ -74,14 +95,9 @@ __global__ __launch_bounds__(64 * WN * WM) void grouped_kernel(GroupedArgs a, ui
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wn = wave % WN, wm = wave / WN;
-  const uint32_t bid = blockIdx.x;
-  const uint32_t per = tiles_total / NXCD, rem = tiles_total % NXCD, xcd = bid % NXCD;
-  const uint32_t t = xcd * per + min(xcd, rem) + bid / NXCD;
-  const uint32_t tm = t / tiles_n;
-  const int32_t n0 = (int32_t)(t - tm * tiles_n) * TN;
-  const Tile tl = find_tile<TM>(a, (int32_t)tm, lane);
+  const Tile tl = find_tile<TM, TN>(a, tiles_n, lane);
   if (tl.m0 >= tl.m1) return;
-  const int32_t N = a.N, K = a.K;
+  const int32_t N = a.N, K = a.K, n0 = tl.n0;
   const int8_t* W = a.w + (int64_t)tl.e * N * K;
 
   // Each thread's 16-byte chunks of a step: LDS chunk id c = tid + i NT holds
@@ -93,7 +109,7 @@ __global__ __launch_bounds__(64 * WN * WM) void grouped_kernel(GroupedArgs a, ui
   {
     const int r = tid / CPR;  // rows of later chunks are r + i NT / CPR: the same swizzle
     static_assert((NT / CPR) % 8 == 0, "the swizzle repeats every 8 rows");
-    kofs = ((tid % CPR) ^ (CPR == 8 ? (r & 6) : (r & 4) >> 1)) * 16;
+    kofs = ((tid % CPR) ^ (r & 6)) * 16;
 #pragma unroll
     for (int i = 0; i < PT; ++i) {
       const int row = r + i * (NT / CPR);
@@ -220,26 +236,44 @@ __global__ __launch_bounds__(64 * WN * WM) void grouped_kernel(GroupedArgs a, ui
   }
 }
 
-template <int WN, int WM, int FI, int FJ, int KB>
+template <int WN, int WM, int FI, int FJ>
 hipError_t launch_cfg(const GroupedArgs& a, hipStream_t s) {
   constexpr int TN = 16 * FI * WN, TM = 16 * FJ * WM;
   const uint32_t tiles_n = (uint32_t)((a.N + TN - 1) / TN);
   const int64_t tiles_m = a.M / TM + (a.E < a.M ? a.E : a.M), total = tiles_m * tiles_n;
-  if (total * 64 * WN * WM >= ((int64_t)1 << 32)) return hipErrorInvalidValue;
+  // total * block < 2^32: the entry point holds (M / 64 + E) (N / 128 + 1) below 2^22,
+  // and the one tile of 1024 threads has E <= M / 192
   const dim3 grid((unsigned)total), block(64 * WN * WM);
   if (a.K % KB == 0)
-    hipLaunchKernelGGL((grouped_kernel<WN, WM, FI, FJ, KB, false>), grid, block, 0, s, a, tiles_n,
-                       (uint32_t)total);
+    hipLaunchKernelGGL((grouped_kernel<WN, WM, FI, FJ, false>), grid, block, 0, s, a, tiles_n);
   else
-    hipLaunchKernelGGL((grouped_kernel<WN, WM, FI, FJ, KB, true>), grid, block, 0, s, a, tiles_n,
-                       (uint32_t)total);
+    hipLaunchKernelGGL((grouped_kernel<WN, WM, FI, FJ, true>), grid, block, 0, s, a, tiles_n);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// Which tile, by M / E rows an expert and by S = M N / 65536, about the number of
+// 256 x 256 tiles; the offsets are on the device, so what an expert really has is
+// not known here.  Times in us at uniformly random experts, int8:
+//   256 x 256, 16 waves (4 a SIMD hide what 1 or 2 cannot: 400 us at 49152 rows of
+//     32 experts, N 2048, K 4096, 2060 Tops; the same tile of 8 waves 405, 128 x 128
+//     of 8 waves 465, of 4 waves 485).  M 12288, E 64, N 4096, K 4096: 270, next 320.
+//     At 96 rows an expert half of it is empty: 250 against 202; with S 96 it
+//     leaves CUs idle: 55 against 40.
+//   128 x 128, 8 waves: M 1536, E 8, N 4096, K 4096: 40 against 58 of 64 rows; with
+//     S 12 it is as good as these, 12.2 against 12.1.
+//   256 channels x 32 rows: weights come in once, at 6.0 TB/s where 64 experts are
+//     2048 x 1024 and have 4 rows each (22 us; 64 rows 26, 128 x 128 27), if two
+//     workgroups a CU can be had: at 8 experts of 4096 x 4096 38 against 34.
+//   128 channels x 64 rows: everything between.
 hipError_t launch_grouped(const GroupedArgs& a, hipStream_t s) {
-  return launch_cfg<2, 2, 4, 4, 128>(a, s);
+  const int64_t size = a.M * a.N, unit = 65536;
+  if (a.M >= 192 * (int64_t)a.E && size > 128 * unit) return launch_cfg<4, 4, 4, 4>(a, s);
+  if (a.M >= 64 * (int64_t)a.E && size >= 24 * unit) return launch_cfg<2, 4, 4, 2>(a, s);
+  if (a.M <= 16 * (int64_t)a.E && a.E * (int64_t)((a.N + 255) / 256) >= 512)
+    return launch_cfg<4, 1, 4, 2>(a, s);
+  return launch_cfg<2, 2, 4, 2>(a, s);
 }
 
 }  // namespace ilw

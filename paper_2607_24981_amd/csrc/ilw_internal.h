@@ -627,6 +627,7 @@ struct AppendArgs {
   int32_t* q_scale;
   int32_t T, seqs, max_new, Hq;
 };
+bool cache_append_fits(const AppendArgs& a);  // one launch can hold it
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s);
 
 struct CacheAttnArgs {
@@ -640,6 +641,7 @@ struct CacheAttnArgs {
   int32_t score_mult, score_t, out_mult, out_shift, causal, window;
   int32_t out_clamp;  // set by launch_cache_attention
 };
+bool cache_attention_fits(const CacheAttnArgs& a);  // its launches can hold it
 size_t cache_attention_workspace(const CacheAttnArgs& a);
 hipError_t launch_cache_attention(const CacheAttnArgs& a, void* ws, hipStream_t s);
 

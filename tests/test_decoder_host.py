@@ -120,6 +120,12 @@ def test_attention_rows_limit():
     assert attention(cache(kv_heads=1), heads=4096, max_q=1 << 20) == E_UNSUP
 
 
+def test_launch_limits():
+    """More workgroups than a launch holds."""
+    assert append(seqs=65535, max_new=1 << 20, tokens=1 << 20) == E_UNSUP
+    assert attention(seqs=65535, max_q=8192, heads=8) == E_UNSUP
+
+
 def grouped(**kw):
     f = dict(x=FAKE, x_rows=10, rows=None, offsets=FAKE, w=FAKE, b=None,
              rq=ilw.Dyadic(FAKE, FAKE, 3 * 32), y=FAKE, M=10, experts=3, N=32, K=64)
@@ -132,7 +138,7 @@ def grouped(**kw):
     (dict(x_rows=0, rows=FAKE), E_SHAPE), (dict(N=24), E_SHAPE), (dict(N=0), E_SHAPE),
     (dict(K=40), E_SHAPE), (dict(K=0), E_SHAPE), (dict(K=131088), E_UNSUP),
     (dict(experts=0), E_SHAPE), (dict(experts=1025), E_SHAPE), (dict(M=1 << 31, x_rows=1 << 31), E_UNSUP),
-    (dict(N=1 << 30), E_UNSUP), (dict(x=None), E_NULL), (dict(w=None), E_NULL),
+    (dict(N=1 << 30), E_UNSUP), (dict(M=1 << 28, x_rows=1 << 28), E_UNSUP), (dict(x=None), E_NULL), (dict(w=None), E_NULL),
     (dict(y=None), E_NULL), (dict(offsets=None), E_NULL), (dict(x=FAKE + 8), E_PARAM),
     (dict(w=FAKE + 4), E_PARAM), (dict(y=FAKE + 2), E_PARAM),
     (dict(rq=ilw.Dyadic(FAKE, FAKE, 32)), E_SHAPE), (dict(rq=ilw.Dyadic(None, FAKE, 1)), E_NULL),

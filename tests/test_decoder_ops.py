@@ -332,3 +332,12 @@ def test_grouped_row_index():
                                         ([2500, 2100], 1040, 1024)])
 def test_grouped_large(counts, N, K):
     run_grouped(rng(N, K), counts, N, K, x_rows=500)
+
+
+# Many rows an expert, rows that fill no tile, and many experts of few rows: the
+# tiles differ; K in whole steps and not.
+@pytest.mark.parametrize("counts,N", [([900, 0, 1189, 0, 3], 4224), ([257] * 2 + [150], 1104),
+                                      ([3] * 171 + [70] + [0] * 84, 528), ([65, 63], 48)])
+@pytest.mark.parametrize("K", [48, 256])
+def test_grouped_tiles(counts, N, K):
+    run_grouped(rng(N, K), counts, N, K, x_rows=200, pad=2)
