@@ -473,9 +473,8 @@ typedef struct {
  * page_size or in pages that are not there, are not appended beyond those
  * limits; query rows are written for the first max_new tokens of each
  * sequence.  Rows outside every sequence are left as they are.  tokens and
- * seqs may be 0.  One launch; no workspace.  A launch holds 2^24 workgroups
- * (each 256/(head_dim/16) groups of 8 query heads, or a page of a kv head's keys
- * or values): more are refused with ILW_E_UNSUPPORTED.
+ * seqs may be 0.  One launch; no workspace.  Calls whose seqs, max_new and heads
+ * need more than a launch's 2^24 workgroups are refused with ILW_E_UNSUPPORTED.
  */
 int ilw_cache_append(const ilw_kv_cache* cache, const int8_t* qkv, int64_t ld,
                      const int32_t* cu_new, const int32_t* past, const int16_t* rope,

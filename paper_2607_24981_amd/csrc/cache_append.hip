@@ -12,18 +12,18 @@
 // the product's high word: a shift, a 64-bit multiply-add and the byte permutes
 // of the packing.
 //
-// Bound: the bytes (a prompt), one round trip through memory after the other (a
-// few tokens).  A team of threads, a wave for a few tokens and four for many,
-// takes the new rows of a (page, kv head), keys and values apart; the queries
-// are groups of D / 16 threads that take a head of 16-channel units each, and
-// several heads of a token one after another so that its cosines are loaded
-// once.
+// Bound: one round trip through memory after the other (a few tokens: 4 us of one
+// sequence, 5 of 64), bytes and the registers that keep them in flight (a prompt
+// of 16384 tokens, 32 + 8 heads of 128: 41 us for the 31 that its 144 MB take to
+// copy).  A team of threads, a wave for a few tokens and two for many, takes the
+// new rows of a (page, kv head), keys and values apart; the queries are groups of
+// D / 16 threads that take a head of 16-channel units each, and several heads of a
+// token one after another so that its cosines are loaded once.
 #include "ilw_internal.h"
 
 namespace ilw {
 namespace {
 
-constexpr int NT = 256;
 
 // Code bytes of values at scale S; see the top of the file.
 struct Codes {
@@ -32,9 +32,13 @@ struct Codes {
   __device__ __forceinline__ void init(int32_t s) {
     S = s;
     const int32_t lg = s > 1 ? 32 - __clz(s - 1) : 0;
-    // the quotient is below 2^27 and at least 2^-17 from the next integer, so
-    // that a rounded double has its floor
-    const int32_t m = (int32_t)((double)((int64_t)1 << (25 + lg)) / (double)s) + 1;
+    // The quotient is below 2^27 and no integer comes within 2^-17 above it: one
+    // Newton step on the hardware's reciprocal (26 bits, then past 50) has its
+    // floor.  Where it is an integer itself (S = 2^lg) one below gives m = the
+    // quotient, no excess at all, and the same codes.
+    const double d = (double)s, r = __builtin_amdgcn_rcp(d);
+    const int32_t m = (int32_t)(__builtin_fma(__builtin_fma(-d, r, 1.0), r, r) *
+                                (double)(1u << (25 + lg - 10)) * 1024.0) + 1;
     sh = 22 - lg;
     m2 = 2 * m;
     c = ((int64_t)257 * s * m) << sh;
@@ -138,6 +142,20 @@ __device__ __forceinline__ uint32_t team_max(uint32_t v, uint32_t* lds) {
   return v;
 }
 
+// The largest of a group of n = 2, 4, 8 or 16 threads (halves that mirror each
+// other: a mirror serves where an exchange would).
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_with(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ uint32_t group_max(uint32_t v, int n) {
+  v = max_with<0xb1>(v);              // quad_perm 1 0 3 2
+  if (n > 2) v = max_with<0x4e>(v);   // quad_perm 2 3 0 1
+  if (n > 4) v = max_with<0x141>(v);  // row_half_mirror
+  if (n > 8) v = max_with<0x140>(v);  // row_mirror
+  return v;
+}
+
 // The page's new scale, from the largest new value and the scale it had.
 __device__ __forceinline__ int32_t page_scale(uint32_t big, bool fresh, int32_t old) {
   const int32_t need = scale_for(big);
@@ -145,42 +163,73 @@ __device__ __forceinline__ int32_t page_scale(uint32_t big, bool fresh, int32_t 
   return need <= old ? old : max(need, old + (old >> 3));
 }
 
-// The new rows lo .. hi - 1 (tokens of the sequence) of one page and kv head,
-// into the rows from slot lo % P on.
+// What a team adds to one page and kv head: the new rows lo .. hi - 1 (tokens of
+// the sequence), into the page's slots from lo - start on.
+struct Part {
+  int32_t block, start, lo, hi;
+  __device__ __forceinline__ bool fresh() const { return lo == start; }
+};
+
+__device__ __forceinline__ bool page_of(const AppendArgs& a, int32_t s, const Part& p,
+                                        int32_t& page) {
+  page = a.c.table[(int64_t)s * a.c.max_pages + p.block];
+  return (uint32_t)page < (uint32_t)a.c.n_pages;
+}
+
+// Two passes over the units, for the scale and with it, in opposite directions:
+// the unit held last is used first, and with one unit a thread (a few tokens)
+// nothing is read twice.  (Holding 2 or 4 units saves no time: 43 and 59
+// us a prompt against 42, at 117 and 128 registers against 70; nor does holding
+// the cosines: 48, at 90.)
 template <int TS>
-__device__ void append_keys(const AppendArgs& a, const Rows& r, int32_t page, int32_t h,
-                            int32_t start, int32_t lo, int32_t hi, int tid, uint32_t* lds) {
-  const int32_t D = a.c.D, upr = D / 16, units = (hi - lo) * upr;
-  const int8_t* src = a.qkv + (int64_t)(a.Hq + h) * D;
-  int8_t* dst = a.c.k + ((((int64_t)page * a.c.Hkv + h) << a.c.lp)) * D;
-  auto values = [&](int u, int32_t(&v)[16], Unit& un) {
-    const int32_t j = lo + u / upr, i = u % upr;
-    un = Unit(i, a.R, a.inter);
-    const int8_t* row = src + (int64_t)(r.first + j - r.past) * a.ld;
-    const u32x2 xa = *(const u32x2*)(row + un.a), xb = *(const u32x2*)(row + un.b);
-    v4i cs[2] = {};
-    if (un.rot) load_rope(a.rope, j, a.R, i, cs);
-    unit_values(xa, xb, cs, un.rot, a.inter, v);
-    return j;
+__device__ void append_keys(const AppendArgs& a, const Rows& r, int32_t s, const Part& p,
+                            int32_t h, int tid, uint32_t* lds) {
+  const int32_t D = a.c.D, upr = D / 16, units = (p.hi - p.lo) * upr;
+  const int8_t* src = a.qkv + (int64_t)(a.Hq + h) * D + (int64_t)(r.first - r.past) * a.ld;
+  u32x2 xa, xb;
+  // unit u: 16 channels of token lo + u / upr
+  auto load = [&](int base) {
+    const int u = base + tid;
+    if (u >= units) return;
+    const int32_t j = p.lo + u / upr, i = u % upr;
+    const Unit un(i, a.R, a.inter);
+    const int8_t* row = src + (int64_t)j * a.ld;
+    xa = *(const u32x2*)(row + un.a);
+    xb = *(const u32x2*)(row + un.b);
   };
+  auto each = [&](int base, auto f) {
+    const int u = base + tid;
+    if (u >= units) return;
+    const Unit un(u % upr, a.R, a.inter);
+    int32_t v[16];
+    v4i cs[2] = {};
+    if (un.rot) load_rope(a.rope, p.lo + u / upr, a.R, u % upr, cs);
+    unit_values(xa, xb, cs, un.rot, a.inter, v);
+    f(p.lo + u / upr, un, v);
+  };
+  load(0);
+  int32_t page;
+  if (!page_of(a, s, p, page)) return;  // (the whole team)
+  int8_t* dst = a.c.k + ((((int64_t)page * a.c.Hkv + h) << a.c.lp)) * D;
   // (read ahead of the barrier, after which the scale may be written)
   int32_t* scale = a.c.k_scale + (int64_t)page * a.c.Hkv + h;
-  const bool fresh = lo == start;
-  const int32_t old = fresh ? 1 : min(max(*scale, 1), 1 << 16);
+  const int32_t old = p.fresh() ? 1 : min(max(*scale, 1), 1 << 16);
   uint32_t big = 0;
-  for (int u = tid; u < units; u += TS) {
-    int32_t v[16];
-    Unit un(0, 0, false);
-    values(u, v, un);
-    big = largest(v, big);
+  auto find = [&](int32_t, const Unit&, int32_t(&v)[16]) { big = largest(v, big); };
+  int base = 0;
+  each(base, find);
+  while (base + TS < units) {
+    base += TS;
+    load(base);
+    each(base, find);
   }
   big = team_max<TS>(big, lds);
-  const int32_t S = page_scale(big, fresh, old);
+  const int32_t S = page_scale(big, p.fresh(), old);
   Codes q;
   q.init(S);
-  if (S != old && !fresh) {
+  if (S != old && !p.fresh()) {
     // (16 codes a step; the rows of a page are consecutive)
-    for (int u = tid; u < (lo - start) * upr; u += TS) {
+    for (int u = tid; u < (p.lo - p.start) * upr; u += TS) {
       v4i w = *(const v4i*)(dst + u * 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -189,29 +238,34 @@ __device__ void append_keys(const AppendArgs& a, const Rows& r, int32_t page, in
       *(v4i*)(dst + u * 16) = w;
     }
   }
-  for (int u = tid; u < units; u += TS) {
-    int32_t v[16];
-    Unit un(0, 0, false);
-    const int32_t j = values(u, v, un);
-    int8_t* row = dst + (int64_t)(j - start) * D;
-    *(u32x2*)(row + un.a) = u32x2{q.pack(v[0], v[1], v[2], v[3]), q.pack(v[4], v[5], v[6], v[7])};
-    *(u32x2*)(row + un.b) =
-        u32x2{q.pack(v[8], v[9], v[10], v[11]), q.pack(v[12], v[13], v[14], v[15])};
+  for (;;) {
+    each(base, [&](int32_t j, const Unit& un, int32_t(&v)[16]) {
+      int8_t* row = dst + (int64_t)(j - p.start) * D;
+      *(u32x2*)(row + un.a) = u32x2{q.pack(v[0], v[1], v[2], v[3]), q.pack(v[4], v[5], v[6], v[7])};
+      *(u32x2*)(row + un.b) =
+          u32x2{q.pack(v[8], v[9], v[10], v[11]), q.pack(v[12], v[13], v[14], v[15])};
+    });
+    if (base == 0) break;
+    base -= TS;
+    load(base);
   }
   if (tid == 0) *scale = S;
 }
 
-// The same of the values, which lie as words of 4 tokens of a channel.  A step
-// takes 4 tokens of 4 channels.
-template <int TS>
-__device__ void append_values(const AppendArgs& a, const Rows& r, int32_t page, int32_t h,
-                              int32_t start, int32_t lo, int32_t hi, int tid, uint32_t* lds) {
+// The same of the values, which lie as words of 4 tokens of a channel, for a few
+// tokens by one wave.  A step takes 4 tokens of 4 channels.
+__device__ void append_few_values(const AppendArgs& a, const Rows& r, int32_t s, const Part& p,
+                                  int32_t h, int tid) {
+  constexpr int TS = 64;
+  const int32_t start = p.start, lo = p.lo, hi = p.hi;
+  int32_t page;
+  if (!page_of(a, s, p, page)) return;  // (the whole wave)
   const int32_t D = a.c.D, wpr = D / 4, P = 1 << a.c.lp, G = min(P, 64);
   const int8_t* src = a.qkv + (int64_t)(a.Hq + a.c.Hkv + h) * D +
                       (int64_t)(r.first - r.past) * a.ld;
   int8_t* dst = a.c.v + ((((int64_t)page * a.c.Hkv + h) << a.c.lp)) * D;
   int32_t* scale = a.c.v_scale + (int64_t)page * a.c.Hkv + h;
-  const bool fresh = lo == start;
+  const bool fresh = p.fresh();
   const int32_t old = fresh ? 1 : min(max(*scale, 1), 1 << 16);
   uint32_t big = 0;
   for (int u = tid; u < (hi - lo) * wpr; u += TS) {
@@ -220,7 +274,7 @@ __device__ void append_values(const AppendArgs& a, const Rows& r, int32_t page, 
 #pragma unroll
     for (int i = 0; i < 4; ++i) big = max(big, (uint32_t)abs(byte_of(w, i)));
   }
-  big = team_max<TS>(big << 14, lds);
+  big = team_max<TS>(big << 14, nullptr);
   const int32_t S = page_scale(big, fresh, old);
   const bool grown = S != old && !fresh;
   Codes q;
@@ -265,9 +319,130 @@ __device__ void append_values(const AppendArgs& a, const Rows& r, int32_t page, 
   if (tid == 0) *scale = S;
 }
 
+// Values of many tokens.  A unit is what 4 channels hold of the tokens j, j + 16,
+// ... of a group that share their j % 16 / 4: M words of 4 tokens of a channel,
+// which lie one after another, and the 4 channels' words do too.  (Units of one
+// word of each channel: every store 64 pieces of 4 bytes, 35 us of values of
+// 16384 tokens and 8 kv heads of 128 against 17.)
+template <int TS>
+__device__ void append_values(const AppendArgs& a, const Rows& r, int32_t s, const Part& p,
+                              int32_t h, int tid, uint32_t* lds) {
+  const int32_t D = a.c.D, wpr = D / 4, P = 1 << a.c.lp, G = min(P, 64), M = G / 16;
+  const int8_t* src = a.qkv + (int64_t)(a.Hq + a.c.Hkv + h) * D +
+                      (int64_t)(r.first - r.past + p.start) * a.ld;
+  const int32_t f = p.lo - p.start, l = p.hi - p.start;  // the new slots f .. l - 1
+  const int32_t g0 = f / G, units = ((l + G - 1) / G - g0) * 4 * wpr;
+  // first slot and channel of a unit, its place in the page
+  struct Place {
+    int32_t s0, c, at;
+  };
+  auto place = [&](int32_t g, int32_t u) {
+    const int32_t jq = u / wpr, c = (u - jq * wpr) * 4;
+    return Place{g * G + jq * 4, c,
+                 g * G * D + (c / 16) * 16 * G + jq * 4 * G + (c % 16) * (G / 4)};
+  };
+  auto unit = [&](int u) {
+    const int32_t g = u / (4 * wpr);
+    return place(g0 + g, u - g * 4 * wpr);
+  };
+  uint32_t x[4][4];  // 4 channels of each token
+  auto load = [&](int base) {
+    const Place q = unit(base + tid);
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int32_t slot = q.s0 + 16 * m + t;
+        x[m][t] = m < M && base + tid < units && slot >= f && slot < l
+                      ? *(const uint32_t*)(src + (int64_t)slot * a.ld + q.c)
+                      : 0;
+      }
+  };
+  load(0);
+  int32_t page;
+  if (!page_of(a, s, p, page)) return;  // (the whole team)
+  int8_t* dst = a.c.v + ((((int64_t)page * a.c.Hkv + h) << a.c.lp)) * D;
+  int32_t* scale = a.c.v_scale + (int64_t)page * a.c.Hkv + h;
+  const int32_t old = p.fresh() ? 1 : min(max(*scale, 1), 1 << 16);
+  int32_t hi = 0, lo = 0;
+  auto find = [&] {
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        hi = max(hi, byte_of(x[k / 4][k % 4], i));
+        lo = min(lo, byte_of(x[k / 4][k % 4], i));
+      }
+  };
+  int base = 0;
+  find();
+  while (base + TS < units) {
+    base += TS;
+    load(base);
+    find();
+  }
+  const uint32_t big = team_max<TS>((uint32_t)max(hi, -lo) << 14, lds);
+  const int32_t S = page_scale(big, p.fresh(), old);
+  const bool grown = S != old && !p.fresh();
+  Codes q;
+  q.init(S);
+  auto requant = [&](uint32_t w) {
+    return q.pack(byte_of(w, 0) * old, byte_of(w, 1) * old, byte_of(w, 2) * old,
+                  byte_of(w, 3) * old);
+  };
+  if (grown) {  // the groups before the new tokens' first
+    for (int u = tid; u < g0 * G * wpr; u += TS) {
+      uint32_t* w = (uint32_t*)dst + u;
+      *w = requant(*w);
+    }
+  }
+  for (;;) {
+    if (base + tid < units) {
+      const Place o = unit(base + tid);
+      int8_t* to = dst + o.at;
+      const bool whole = o.s0 >= f && o.s0 + G - 12 <= l;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t w[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          w[m] = q.pack((int32_t)((uint32_t)byte_of(x[m][0], i) << 14),
+                        (int32_t)((uint32_t)byte_of(x[m][1], i) << 14),
+                        (int32_t)((uint32_t)byte_of(x[m][2], i) << 14),
+                        (int32_t)((uint32_t)byte_of(x[m][3], i) << 14));
+        uint32_t* d = (uint32_t*)(to + i * (G / 4));
+        if (whole && M == 4) {
+          *(v4i*)d = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+          continue;
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const int32_t s0 = o.s0 + 16 * m;
+          // words without new tokens change only where the scale grew, and only
+          // in tokens before the new ones
+          if (m >= M || s0 >= l || (s0 + 4 <= f && !grown)) continue;
+          uint32_t v = w[m];
+          if (s0 < f || s0 + 4 > l) {
+            const uint32_t was = d[m], keep = grown ? requant(was) : was;
+            v = 0;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+              v |= 0xffu << (8 * t) & (s0 + t < f ? keep : s0 + t < l ? w[m] : was);
+          }
+          d[m] = v;
+        }
+      }
+    }
+    if (base == 0) break;
+    base -= TS;
+    load(base);
+  }
+  if (tid == 0) *scale = S;
+}
+
 // Blocks 0 .. kv_blocks - 1: teams of TS threads, one for each (sequence, page
 // of those it may write, kv head, keys or values).  The others: the queries.
-template <int TS>
+template <int TS, int NT>
 __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a, uint32_t nb, uint32_t kv_units,
                                                     uint32_t kv_blocks, int32_t hpu,
                                                     uint32_t q_blocks) {
@@ -279,15 +454,17 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a, uint32_t nb, u
     const uint32_t heads = 2 * (uint32_t)a.c.Hkv, sb = unit / heads, hv = unit - sb * heads;
     const int32_t s = (int32_t)(sb / nb), b = (int32_t)(sb - (uint32_t)s * nb);
     const Rows r(a, s);
-    const int32_t P = 1 << a.c.lp, block = (r.past >> a.c.lp) + b, start = block << a.c.lp;
-    const int32_t lo = max(r.past, start), hi = min(r.past + r.n, start + P);
-    if (lo >= hi || block >= a.c.max_pages) return;
-    const int32_t page = a.c.table[(int64_t)s * a.c.max_pages + block];
-    if ((uint32_t)page >= (uint32_t)a.c.n_pages) return;
+    Part p;
+    p.block = (r.past >> a.c.lp) + b;
+    p.start = p.block << a.c.lp;
+    p.lo = max(r.past, p.start);
+    p.hi = min(r.past + r.n, p.start + (1 << a.c.lp));
+    if (p.lo >= p.hi || p.block >= a.c.max_pages) return;
     const int tid = threadIdx.x % TS;
     const int32_t h = (int32_t)(hv >> 1);
-    if (hv & 1) append_values<TS>(a, r, page, h, start, lo, hi, tid, lds);
-    else append_keys<TS>(a, r, page, h, start, lo, hi, tid, lds);
+    if (!(hv & 1)) append_keys<TS>(a, r, s, p, h, tid, lds);
+    else if constexpr (TS == 64) append_few_values(a, r, s, p, h, tid);
+    else append_values<TS>(a, r, s, p, h, tid, lds);
     return;
   }
   // queries: a group of D / 16 threads takes hpu heads of one token
@@ -305,12 +482,18 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendArgs a, uint32_t nb, u
   const int8_t* row = a.qkv + t * a.ld;
   v4i cs[2] = {};
   if (un.rot) load_rope(a.rope, pos, a.R, un_i, cs);
-  for (int32_t h = h0; h < min(h0 + hpu, a.Hq); ++h) {
-    const u32x2 xa = *(const u32x2*)(row + h * D + un.a), xb = *(const u32x2*)(row + h * D + un.b);
+  const int32_t h1 = min(h0 + hpu, a.Hq);
+  u32x2 na = *(const u32x2*)(row + h0 * D + un.a), nb2 = *(const u32x2*)(row + h0 * D + un.b);
+  for (int32_t h = h0; h < h1; ++h) {
+    const u32x2 xa = na, xb = nb2;
+    if (h + 1 < h1) {  // the next head's, while this one is worked on
+      na = *(const u32x2*)(row + (h + 1) * D + un.a);
+      nb2 = *(const u32x2*)(row + (h + 1) * D + un.b);
+    }
     int32_t v[16];
     unit_values(xa, xb, cs, un.rot, a.inter, v);
     uint32_t big = largest(v, 0);
-    for (int o = 1; o < upr; o <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o, 64));
+    big = group_max(big, upr);
     Codes q;
     q.init(scale_for(big));
     int8_t* dst = a.q + (t * a.Hq + h) * D;
@@ -327,7 +510,7 @@ namespace {
 
 struct Grid {
   bool few;
-  int32_t hpu;
+  int32_t hpu, NT;
   int64_t nb, units, kv_blocks, q_blocks, total;
   explicit Grid(const AppendArgs& a) {
     const int32_t P = 1 << a.c.lp;
@@ -338,6 +521,7 @@ struct Grid {
     few = a.max_new <= 8;
     kv_blocks = few ? (units + 3) / 4 : units;
     hpu = few ? 1 : 8;
+    NT = few ? 256 : 128;
     const int32_t groups = (a.Hq + hpu - 1) / hpu, per = NT / (a.c.D / 16);
     q_blocks = ((int64_t)a.max_new * groups + per - 1) / per;
     total = kv_blocks + q_blocks * a.seqs;
@@ -351,11 +535,11 @@ bool cache_append_fits(const AppendArgs& a) { return Grid(a).total < ((int64_t)1
 hipError_t launch_cache_append(const AppendArgs& a, hipStream_t s) {
   const Grid g(a);
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)g.total), dim3(NT), 0, s, a, (uint32_t)g.nb,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)g.total), dim3(g.NT), 0, s, a, (uint32_t)g.nb,
                        (uint32_t)g.units, (uint32_t)g.kv_blocks, g.hpu, (uint32_t)g.q_blocks);
     return hipGetLastError();
   };
-  return g.few ? launch(append_kernel<64>) : launch(append_kernel<256>);
+  return g.few ? launch(append_kernel<64, 256>) : launch(append_kernel<128, 128>);
 }
 
 }  // namespace ilw
