@@ -341,3 +341,296 @@ def test_grouped_large(counts, N, K):
 @pytest.mark.parametrize("K", [48, 256])
 def test_grouped_tiles(counts, N, K):
     run_grouped(rng(N, K), counts, N, K, x_rows=200, pad=2)
+
+
+# ------------------------------------------------------------- larger numbers
+def scattered(g, seqs, max_pages, hk, P, D, n=40):
+    """A small pool that long sequences name again and again."""
+    c = make_cache(g, 1, n, hk, P, D, spare=0)
+    c["table"] = g.integers(0, n, (seqs, max_pages)).astype(np.int32)
+    return c
+
+
+@pytest.mark.parametrize("D,P", [(32, 64), (64, 16), (128, 64), (256, 32)])
+def test_attention_many_rows_steep(D, P):
+    """Scores far past 16 bits before they are clamped, by the rows of prompts."""
+    hk, heads, seqs = 4, 8, 60
+    g = rng(D, P, 5)
+    p = params(D, 60.0 * np.sqrt(D))  # a ninth below what is refused
+    assert (33026 * p["score_mult"] >> (p["score_shift"] - 16)) * 37154 >> 16 >= 1 << 27
+    c = make_cache(g, seqs, -(-200 // P), hk, P, D)
+    c["k_scale"][::3] = 37154
+    new = [40, 33] + [int(x) for x in g.integers(0, 4, seqs - 2)]
+    lens = [200, 20] + [int(x) for x in g.integers(0, 100, seqs - 2)]
+    run_attention(c, heads, new, lens, p, True, 0, f"steep D={D} P={P}", g=g)
+
+
+@pytest.mark.parametrize("max_len", [131072, 131072 + 256])
+@pytest.mark.parametrize("flat", [False, True])
+def test_attention_long_prompt(max_len, flat):
+    """The longest sequence whose sums one kernel takes, and one that is split;
+    flat scores give the largest sums there are."""
+    D, P, hk, heads, seqs = 32, 256, 4, 4, 48
+    g = rng(max_len, flat)
+    c = scattered(g, seqs, max_len // P, hk, P, D)
+    p = params(D)
+    if flat:
+        p["score_mult"] = 0
+        c["v"][:] = np.where(g.integers(0, 20, c["v"].shape) > 0, -127, 127)
+        c["v_scale"][:] = 18577
+    new = [3, 66] + [1] * (seqs - 2)
+    lens = [max_len, 70] + [int(x) for x in g.integers(0, 90, seqs - 2)]
+    run_attention(c, heads, new, lens, p, True, 0, f"long prompt {max_len} flat={flat}", g=g)
+
+
+def test_pool_past_32_bits():
+    """Pages whose bytes lie past 2^32 of the pools."""
+    D, P, hk, heads, seqs, max_pages = 64, 256, 1, 2, 3, 13
+    n = (1 << 32) // (P * D * hk) + 64
+    g = rng(12)
+    c = make_cache(g, seqs, max_pages, hk, P, D, spare=0)
+    used = c["k"].shape[0]
+    say(f"pools of {n * hk * P * D} bytes")
+    big = {"k": torch.empty((n, hk, P, D), dtype=torch.int8, device="cuda"),
+           "v": torch.empty((n, hk, P, D), dtype=torch.int8, device="cuda"),
+           "k_scale": torch.ones((n, hk), dtype=torch.int32, device="cuda"),
+           "v_scale": torch.ones((n, hk), dtype=torch.int32, device="cuda")}
+    for name, t in big.items():
+        t[n - used:] = dev(c[name])
+    cache = ilw.KVCache(big["k"], big["v"], big["k_scale"], big["v_scale"],
+                        dev(c["table"] + (n - used)))
+    rope = rope_of(max_pages * P, D)
+    for new, past in [([1, 0, 1], [2500, 0, 255]), ([30, 290, 11], [3000, 200, 0])]:
+        T = sum(new)
+        cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        qkv = g.integers(-127, 128, (T, (heads + 2 * hk) * D)).astype(np.int8)
+        q, qs = ilw.ilw_cache_append(cache, dev(qkv), heads, dev(cu), dev(np.array(past, np.int32)),
+                                     max(new), rope=dev(rope))
+        want_q, want_s = np.zeros((T, heads, D), np.int8), np.zeros((T, heads), np.int32)
+        plain.append(c, qkv, heads, cu.tolist(), past, max(new), rope, False, want_q, want_s)
+        same(q, want_q, "q")
+        for name in big:
+            same(big[name][n - used:], c[name], name)
+        lens = [a + b for a, b in zip(new, past)]
+        out = ilw.ilw_cache_attention(cache, q, qs, dev(cu), dev(np.array(lens, np.int32)),
+                                      params(D), max(new), max(lens))
+        want = np.zeros((T, heads, D), np.int8)
+        plain.attention(c, want_q, want_s, cu.tolist(), lens, params(D), max(new), max(lens), True,
+                        0, want)
+        same(out.view(T, heads, D), want, "attention")
+
+
+def test_grouped_past_32_bits():
+    """An output and weights of more than 2^31 and 2^32 bytes; the last rows."""
+    for M, E, N, K in [(70000, 2, 32768, 16), (1200, 1024, 1024, 4112)]:
+        say(f"grouped M={M} E={E} N={N} K={K}")
+        g = rng(M, N)
+        w = torch.randint(-127, 128, (E, N, K), dtype=torch.int8, device="cuda")
+        x = g.integers(-127, 128, (M, K)).astype(np.int8)
+        cut = M - 9 if E == 2 else M - E
+        off = np.array([0, cut, M] if E == 2 else [0] + [cut + 1 + e for e in range(E)], np.int32)
+        mult, shift = np.array([1 << 29], np.int32), np.array([38], np.int32)
+        y = ilw.ilw_linear_grouped(dev(x), w, dev(off), None, dev(mult), dev(shift))
+        rows = [cut - 1, cut, cut + 1, M - 1]
+        for r in rows:
+            e = int(np.searchsorted(off, r, side="right")) - 1
+            want = np.zeros((1, N), np.int8)
+            plain.grouped(x[r:r + 1], None, [0, 1], w[e:e + 1].cpu().numpy(), None, mult, shift, want)
+            same(y[r:r + 1], want, f"row {r}")
+        del w, y
+
+
+# ---------------------------------------------- as they are used, one after another
+class Layer:
+    """A decoder layer with experts: linear, append, attention, linear, experts
+    up, GELU, experts down; every step's input is the step before."""
+
+    def __init__(self, g, hidden=128, heads=4, hk=2, D=64, E=5, ffn=96):
+        def lin(n, k, e=None):
+            shape = (n, k) if e is None else (e, n, k)
+            w = g.integers(-127, 128, shape).astype(np.int8)
+            b = g.integers(-2 ** 12, 2 ** 12, shape[:-1]).astype(np.int32)
+            # (73^2 sqrt(k) of an accumulator to about 42 of a code)
+            rq = 42 / (73.0 * 73.0 * np.sqrt(k)) * g.uniform(0.9, 1.1, shape[:-1])
+            return w, b, np.rint(rq * 2.0 ** 38).astype(np.int32), np.full(shape[:-1], 38, np.int32)
+        self.heads, self.hk, self.D = heads, hk, D
+        self.host = {"qkv": lin((heads + 2 * hk) * D, hidden), "out": lin(hidden, heads * D),
+                     "up": lin(ffn, hidden, E), "down": lin(hidden, ffn, E)}
+        self.dev = {k: [dev(a) for a in v] for k, v in self.host.items()}
+        self.params = params(D)
+        self.rope = rope_of(4096, D)
+        self.dev_rope = dev(self.rope)
+
+    def run(self, cache, x, cu, past, lens, max_new, max_len, rows, offsets):
+        d = self.dev
+        w, b, m, s = d["qkv"]
+        t = {"qkv": ilw.ilw_linear(x, w, b, m, s)}
+        t["q"], t["qs"] = ilw.ilw_cache_append(cache, t["qkv"], self.heads, cu, past, max_new,
+                                               rope=self.dev_rope)
+        t["att"] = ilw.ilw_cache_attention(cache, t["q"], t["qs"], cu, lens, self.params, max_new,
+                                           max_len)
+        w, b, m, s = d["out"]
+        t["out"] = ilw.ilw_linear(t["att"], w, b, m, s)
+        w, b, m, s = d["up"]
+        t["up"] = ilw.ilw_linear_grouped(t["out"], w, offsets, b, m, s, rows=rows)
+        t["act"] = ilw.ilw_sdshiftgelu(t["up"], 50, 1 << 30, 37)
+        w, b, m, s = d["down"]
+        t["down"] = ilw.ilw_linear_grouped(t["act"], w, offsets, b, m, s)
+        return t
+
+    def check(self, c, t, x, cu, past, lens, max_new, max_len, rows, offsets):
+        """Every step but GELU (tested elsewhere) from the step before."""
+        T = len(x)
+
+        def grouped(x, rows, offsets, p):
+            w, b, m, s = [a if a.ndim > 1 and len(a) == len(offsets) - 1 else a[None] for a in p]
+            y = np.zeros((int(offsets[-1]), w.shape[1]), np.int8)
+            plain.grouped(x, rows, offsets, w, b, m, s, y)
+            return y
+        h = {k: v.cpu().numpy() for k, v in t.items()}
+        same(t["qkv"], grouped(x, None, [0, T], self.host["qkv"]), "qkv")
+        q, qs = np.zeros((T, self.heads, self.D), np.int8), np.zeros((T, self.heads), np.int32)
+        plain.append(c, h["qkv"], self.heads, cu.tolist(), past.tolist(), max_new, self.rope, False,
+                     q, qs)
+        same(t["q"], q, "q")
+        same(t["qs"], qs, "q_scale")
+        att = np.zeros_like(q)
+        plain.attention(c, q, qs, cu.tolist(), lens.tolist(), self.params, max_new, max_len, True, 0,
+                        att)
+        same(t["att"], att.reshape(T, -1), "attention")
+        same(t["out"], grouped(h["att"], None, [0, T], self.host["out"]), "out")
+        same(t["up"], grouped(h["out"], rows, offsets, self.host["up"]), "up")
+        same(t["down"], grouped(h["act"], None, offsets, self.host["down"]), "down")
+        assert h["down"].any()
+
+
+def route(g, T, E, each=2):
+    """Rows of T tokens sorted by expert, `each` experts a token."""
+    e = np.stack([g.permutation(E)[:each] for _ in range(T)])
+    order = np.argsort(e.reshape(-1), kind="stable")
+    offsets = np.concatenate([[0], np.cumsum(np.bincount(e.reshape(-1), minlength=E))])
+    return (order // each).astype(np.int32), offsets.astype(np.int32)
+
+
+def test_decoder_layer_prompt_then_tokens():
+    """A prompt, a second piece of it, then tokens one by one."""
+    g = rng(21)
+    L = Layer(g)
+    c = make_cache(g, 3, 20, L.hk, 16, L.D)
+    cache = on_device(c)
+    past = np.zeros(3, np.int32)
+    for new in [[130, 1, 17], [20, 40, 1]] + [[1, 1, 1]] * 4 + [[0, 2, 1]]:
+        say(f"layer {new}")
+        T, n = sum(new), np.array(new, np.int32)
+        cu = np.concatenate([[0], np.cumsum(n)]).astype(np.int32)
+        x = g.integers(-127, 128, (T, 128)).astype(np.int8)
+        rows, offsets = route(g, T, 5)
+        lens = past + n
+        args = (cu, past, lens)
+        t = L.run(cache, dev(x), *[dev(a) for a in args], max(new), int(lens.max()), dev(rows),
+                  dev(offsets))
+        L.check(c, t, x, *args, max(new), int(lens.max()), rows, offsets)
+        same_cache(cache, c, "cache")
+        past = lens
+
+
+@pytest.mark.parametrize("max_len", [320, 4000])
+def test_decoder_layer_captured(max_len):
+    """One token of each sequence as a graph, replayed with other inputs and
+    lengths in the same arrays, eager work between the replays; the attention is
+    one launch (320) or three over a workspace of the graph's (4000)."""
+    g = rng(22, max_len)
+    L = Layer(g)
+    seqs, P = 3, 16
+    c = make_cache(g, seqs, max_len // P, L.hk, P, L.D)
+    lens0 = np.array([max_len - 20, 5, max_len // 2], np.int32)
+    cache, other = on_device(c), on_device(c)
+    x = torch.zeros((seqs, 128), dtype=torch.int8, device="cuda")
+    cu = dev(np.arange(seqs + 1, dtype=np.int32))
+    past, lens = dev(lens0), dev(lens0 + 1)
+    rows, offsets = [dev(a) for a in route(g, seqs, 5)]
+    args = (cu, past, lens, 1, max_len, rows, offsets)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        L.run(cache, x, *args)  # (whatever a first call sets up)
+    torch.cuda.current_stream().wait_stream(s)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        getattr(cache, name).copy_(dev(c[name]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        t = L.run(cache, x, *args)
+    for i in range(5):
+        say(f"replay {i}")
+        xi = g.integers(-127, 128, (seqs, 128)).astype(np.int8)
+        r, o = route(g, seqs, 5)
+        x.copy_(dev(xi))
+        past.copy_(dev(lens0 + i))
+        lens.copy_(dev(lens0 + i + 1))
+        rows.copy_(dev(r))
+        offsets.copy_(dev(o))
+        graph.replay()
+        eager = L.run(other, dev(xi), cu, dev(lens0 + i), dev(lens0 + i + 1), 1, max_len, dev(r), dev(o))
+        torch.cuda.synchronize()
+        for k in t:
+            assert torch.equal(t[k], eager[k]), (i, k)
+        for k in ("k", "v", "k_scale", "v_scale"):
+            assert torch.equal(getattr(cache, k), getattr(other, k)), (i, k)
+        L.check(c, t, xi, np.arange(seqs + 1), lens0 + i, lens0 + i + 1, 1, max_len, r, o)
+
+
+def test_streams_side_by_side():
+    """Two layers on two streams, neither the default one, each its own cache;
+    inputs written on the stream that reads them."""
+    g = rng(23)
+    L = Layer(g)
+    runs = []
+    for i in range(2):
+        c = make_cache(g, 2, 250, L.hk, 16, L.D)
+        x = g.integers(-127, 128, (2, 128)).astype(np.int8)
+        lens = np.array([3900, 60 + i], np.int32)
+        rows, offsets = route(g, 2, 5)
+        runs.append(dict(c=c, cache=on_device(c), x=x, lens=lens, rows=rows, offsets=offsets,
+                         stream=torch.cuda.Stream()))
+    cu = np.arange(3, dtype=np.int32)
+    dcu = dev(cu)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for r in runs:
+            with torch.cuda.stream(r["stream"]):
+                x = torch.zeros((2, 128), dtype=torch.int8, device="cuda")
+                x += dev(r["x"])
+                # (the token at lens - 1 is appended again, with what it had)
+                r["t"] = L.run(r["cache"], x, dcu, dev(r["lens"] - 1), dev(r["lens"]), 1, 4000,
+                               dev(r["rows"]), dev(r["offsets"]))
+                r["keep"] = x
+    torch.cuda.synchronize()
+    for r in runs:
+        for _ in range(2):  # the plain cache takes the same three appends
+            plain.append(r["c"], r["t"]["qkv"].cpu().numpy(), L.heads, cu.tolist(),
+                         (r["lens"] - 1).tolist(), 1, L.rope, False,
+                         np.zeros((2, L.heads, L.D), np.int8), np.zeros((2, L.heads), np.int32))
+        L.check(r["c"], r["t"], r["x"], cu, r["lens"] - 1, r["lens"], 1, 4000, r["rows"], r["offsets"])
+
+
+@pytest.mark.parametrize("fill", [0, 0x7f, 0xff])
+def test_workspace_of_any_content(fill):
+    """A workspace of exactly the size asked for, holding anything."""
+    D, P, heads, hk = 128, 64, 6, 2
+    g = rng(24)
+    c = make_cache(g, 2, 50, hk, P, D)
+    c["table"][0, 3] = -1
+    lens, new = [3100, 700], [2, 2]
+    q = g.integers(-127, 128, (4, heads, D)).astype(np.int8)
+    qs = g.integers(9000, 21000, (4, heads)).astype(np.int32)
+    cache = on_device(c)
+    need = ilw.lib().ilw_cache_attention_workspace_bytes(cache.struct, 2, 2, 3200, heads, 0)
+    assert need > 0
+    buf = torch.full((need + 512,), fill, dtype=torch.uint8, device="cuda")
+    out = ilw.ilw_cache_attention(cache, dev(q), dev(qs), dev(np.array([0, 2, 4], np.int32)),
+                                  dev(np.array(lens, np.int32)), params(D), 2, 3200,
+                                  workspace=buf[256:256 + need].view(torch.int8))
+    want = np.zeros((4, heads, D), np.int8)
+    plain.attention(c, q, qs, [0, 2, 4], lens, params(D), 2, 3200, True, 0, want)
+    same(out.view(4, heads, D), want, "attention")
+    assert bool((buf[:256] == fill).all()) and bool((buf[256 + need:] == fill).all())
