@@ -432,7 +432,7 @@ int ilw_decoder_layer(const ilw_decoder_params* p, const int8_t* tgt, const int8
  * All are DEVICE pointers, k and v 16-byte aligned; page_size 16, 32, 64, 128
  * or 256; head_dim 32, 64, 128 or 256; max_pages * page_size <= 2^20.  The struct
  * is read during the call.  Two sequences may share pages that neither
- * appends to; a page that one call appends to belongs to one sequence of it.
+ * appends to; a page that one call appends to is named once, by one sequence.
  */
 typedef struct {
   int8_t* k;

@@ -38,7 +38,8 @@ FLAGS = ["-O3", f"--offload-arch={ARCH}", "-std=c++17", "-fPIC", "-Wall",
 # accumulation-register form costs one copy per value.  The split convolution's
 # 64 x 64 tiles drop from 132 registers to 118, one more wave per SIMD (16 384
 # tokens of 4 x 192 channels to 256: 18.9 -> 13.9 us; 3072 tokens to 384: 10.1
-# -> 9.2 us); the GEMM tiles measured the same either way.
+# -> 9.2 us); the GEMM tiles measured the same either way.  The cache attention's
+# scores and digit sums are of the same kind.
 SOURCE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"]
                 for src in ("attention.hip", "split_conv.hip", "cache_attention.hip")}
 
