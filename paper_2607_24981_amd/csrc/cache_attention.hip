@@ -634,33 +634,42 @@ __device__ __forceinline__ int32_t few_scores(const CacheAttnArgs& a, const Rows
   Pages<GB> p0 = list.at(a.c, h, kb0, lane);
   Keys<D> k0;
   k0.load(a.c, p0, h, kb0, lane);
-  for (int32_t kb = kb0; kb < c1; kb += 64 * NW) {
-    list.scale(a.c, kb, p0);
+  // one step from pg and k, the next one's page and keys on their way to pn and kn
+  auto step = [&](int32_t kb, Pages<GB>& pg, const Keys<D>& k, Pages<GB>& pn, Keys<D>& kn) {
+    list.scale(a.c, kb, pg);
     // (past the last step too: any page number leads to a page)
-    const Pages<GB> p1 = list.at(a.c, h, kb + 64 * NW, lane);
-    Keys<D> k1;
-    k1.load(a.c, p1, h, kb + 64 * NW, lane);
-    const bool fast = kb >= R.all_lo && kb + 64 <= R.all_hi && p0.all();
+    pn = list.at(a.c, h, kb + 64 * NW, lane);
+    kn.load(a.c, pn, h, kb + 64 * NW, lane);
     v4i w[2];
+    auto scores = [&](auto checked) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const v4i p = R.products(k0, u, 0);
-      const int32_t m = score_mult(R.A[0], p0.ks[u / GB]);
-      int32_t x[4];
+      for (int u = 0; u < 4; ++u) {
+        const v4i p = R.products(k, u, 0);
+        const int32_t m = score_mult(R.A[0], pg.ks[u / GB]);
+        int32_t x[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        x[r] = med3(rescale(p[r], m, kRnd), -32767, 32767);
-        if (!fast && !R.sees(0, kb + 16 * u + 4 * (lane >> 4) + r, p0.ks[u / GB])) x[r] = kNone;
-        M = max(M, x[r]);
+        for (int r = 0; r < 4; ++r) {
+          x[r] = med3(rescale(p[r], m, kRnd), -32767, 32767);
+          if (decltype(checked)::value)
+            x[r] = R.sees(0, kb + 16 * u + 4 * (lane >> 4) + r, pg.ks[u / GB]) ? x[r] : kNone;
+          M = max(M, x[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          w[u / 2][(u % 2) * 2 + r] = (int)__builtin_amdgcn_perm((uint32_t)x[2 * r + 1],
+                                                                 (uint32_t)x[2 * r], 0x05040100u);
       }
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-        w[u / 2][(u % 2) * 2 + r] = (int)__builtin_amdgcn_perm((uint32_t)x[2 * r + 1],
-                                                               (uint32_t)x[2 * r], 0x05040100u);
-    }
+    };
+    if (kb >= R.all_lo && kb + 64 <= R.all_hi && pg.all()) scores(Flag<false>{});
+    else scores(Flag<true>{});
     out(kb >> 6, w);
-    p0 = p1;
-    k0 = k1;
+  };
+  Pages<GB> p1;
+  Keys<D> k1;
+  for (int32_t kb = kb0; kb < c1; kb += 128 * NW) {
+    step(kb, p0, k0, p1, k1);
+    if (kb + 64 * NW >= c1) break;
+    step(kb + 64 * NW, p1, k1, p0, k0);
   }
   return M;
 }
@@ -672,55 +681,79 @@ template <int D, int GB, int NW, typename Top, typename In>
 __device__ __forceinline__ uint32_t few_values(const CacheAttnArgs& a, PageList<GB> list, int32_t h,
                                                int32_t c0, int32_t c1, int wave, int lane, Top top,
                                                In in, v4i (&oh)[D / 16], v4i (&ol)[D / 16]) {
+  // values are loaded a step ahead where registers are left for a second set (with
+  // 256 channels that spilled: 700 keys 26 us so, 16 now; 8 x 16384 keys 29 and 22)
+  constexpr bool AHEAD = D < 256;
   constexpr int CG = D / 16;
   uint32_t L = 0;
   const v4i zero = {0, 0, 0, 0};
 #pragma unroll
   for (int g = 0; g < CG; ++g) oh[g] = ol[g] = zero;
   const int32_t kb0 = c0 + wave * 64;
+  auto load = [&](const Pages<GB>& pg, int32_t kb, v4i(&v)[CG]) {
+#pragma unroll
+    for (int g = 0; g < CG; ++g) v[g] = load_values<D, GB>(a.c, pg, h, kb, g, lane);
+  };
   Pages<GB> p0;
   v4i v0[CG];
   if (kb0 < c1) {
     list.start(a.c, h, kb0, lane);
     p0 = list.at(a.c, h, kb0, lane);
-#pragma unroll
-    for (int g = 0; g < CG; ++g) v0[g] = load_values<D, GB>(a.c, p0, h, kb0, g, lane);
+    load(p0, kb0, v0);
   }
   // (a wave's own scores: no other wave's are read)
   v4i x0[2];
   if (kb0 < c1) in(kb0 >> 6, x0);
   const Ref ref = top();
-  for (int32_t kb = kb0; kb < c1; kb += 64 * NW) {
-    v4i v1[CG], x1[2], ph, pl;
-    if (kb + 64 * NW < c1) in((kb >> 6) + NW, x1);
-    list.scale(a.c, kb, p0);
-    const Pages<GB> p1 = list.at(a.c, h, kb + 64 * NW, lane);
-#pragma unroll
-    for (int g = 0; g < CG; ++g) v1[g] = load_values<D, GB>(a.c, p1, h, kb + 64 * NW, g, lane);
+  auto step = [&](int32_t kb, Pages<GB>& pg, v4i(&v)[CG], const v4i(&x)[2], Pages<GB>& pn,
+                  v4i(&vn)[CG], v4i(&xn)[2]) {
+    if (kb + 64 * NW < c1) in((kb >> 6) + NW, xn);
+    list.scale(a.c, kb, pg);
+    if (!AHEAD && kb != kb0) load(pg, kb, v);
+    pn = list.at(a.c, h, kb + 64 * NW, lane);
+    if (AHEAD) load(pn, kb + 64 * NW, vn);
+    v4i ph, pl;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       uint32_t w[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int32_t two = x0[u / 2][(u % 2) * 2 + r / 2];
+        const int32_t two = x[u / 2][(u % 2) * 2 + r / 2];
         const int32_t sc = r % 2 ? two >> 16 : (int16_t)two;
-        w[r] = sc == kNone ? 0 : weight(med3(sc - ref.m, ref.cap, 0));
+        // (made for all of them: a choice between 0 and what inline asm has part in
+        // becomes a branch, 16 a step: 700 keys of 64 channels 8.1 us so, 7.0 now)
+        const uint32_t all = weight(med3(sc - ref.m, ref.cap, 0));
+        w[r] = sc == kNone ? 0 : all;
       }
       L += w[0] + w[1] + w[2] + w[3];
-      const Digits d(w, (uint32_t)p0.vs[u / GB]);
+      const Digits d(w, (uint32_t)pg.vs[u / GB]);
       ph[u] = (int)d.hi;
       pl[u] = (int)d.lo;
     }
 #pragma unroll
     for (int g = 0; g < CG; ++g) {
-      oh[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v0[g], ph, oh[g], 0, 0, 0);
-      ol[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v0[g], pl, ol[g], 0, 0, 0);
+      oh[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[g], ph, oh[g], 0, 0, 0);
+      ol[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v[g], pl, ol[g], 0, 0, 0);
     }
-    p0 = p1;
-    x0[0] = x1[0];
-    x0[1] = x1[1];
-#pragma unroll
-    for (int g = 0; g < CG; ++g) v0[g] = v1[g];
+  };
+  if constexpr (AHEAD) {
+    Pages<GB> p1;
+    v4i v1[CG], x1[2];
+    for (int32_t kb = kb0; kb < c1; kb += 128 * NW) {
+      step(kb, p0, v0, x0, p1, v1, x1);
+      if (kb + 64 * NW >= c1) break;
+      step(kb + 64 * NW, p1, v1, x1, p0, v0, x0);
+    }
+  } else {
+#pragma unroll 1
+    for (int32_t kb = kb0; kb < c1; kb += 64 * NW) {
+      Pages<GB> p1;
+      v4i x1[2];
+      step(kb, p0, v0, x0, p1, v0, x1);
+      p0 = p1;
+      x0[0] = x1[0];
+      x0[1] = x1[1];
+    }
   }
   return L;
 }
