@@ -512,11 +512,12 @@ int ilw_cache_append(const ilw_kv_cache* cache, const int8_t* qkv, int64_t ld,
  * past max_len are not there.  max_len <= max_pages * page_size.
  * q_scale in [1, 33026], page scales in [1, 37154] (keys) and [1, 18577]
  * (values), which ilw_cache_append keeps to.  The workspace may hold anything.
- * Its size is that of the call's seqs, max_q, max_len, heads and window; where
- * few rows or more than 131072 keys are split over the machine it holds two
- * bytes for each query row and key, so that a prompt longer than that is given
- * in pieces.  Calls whose rows need more than a launch's 2^32 threads are
- * refused with ILW_E_UNSUPPORTED.
+ * Its size follows from the call's seqs, max_q, max_len, heads and window and may
+ * be 0; where few rows or more than 131072 keys are split over the machine it
+ * holds two bytes for each query row and key, so that a prompt longer than that is
+ * given in pieces.  Calls that may run at the same time need a workspace each.
+ * Calls whose rows need more than a launch's 2^32 threads are refused with
+ * ILW_E_UNSUPPORTED.
  */
 typedef struct {
   int32_t score_mult, score_shift;

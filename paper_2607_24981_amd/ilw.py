@@ -596,13 +596,16 @@ def ilw_deform_attn_boxes(value, level_hw, level_start, ref, offsets, logits, I0
                    logits, I0, out_mult, out_shift, mode, s_d, out, k_inter, k_out, m_p)
 
 
+_Tensor = torch.Tensor
+
+
 def _device(t, name) -> int:
     """Index of the device that a call goes to: t's, which has to be the current
     one (calls are issued on its current stream)."""
-    d = t.get_device() if isinstance(t, torch.Tensor) else -1
+    d = t.get_device() if isinstance(t, _Tensor) else -1
     if d < 0:
         raise IlwError(f"{name} must be a device tensor")
-    if d != torch.cuda.current_device():
+    if d != torch._C._cuda_getDevice():  # (the device is up: it holds a tensor)
         raise IlwError(f"{name} is on cuda:{d}, and cuda:{torch.cuda.current_device()} is the "
                        "current device")
     return d
@@ -610,13 +613,14 @@ def _device(t, name) -> int:
 
 def _at(t, dtype, name, device) -> int:
     """Address of a contiguous tensor of that type on that device."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+    if (isinstance(t, _Tensor) and t.dtype is dtype and t.get_device() == device
+            and t.is_contiguous()):
+        return t.data_ptr()
+    if not isinstance(t, _Tensor) or t.get_device() != device:
         raise IlwError(f"{name} must be a tensor on cuda:{device}")
     if t.dtype is not dtype:
         raise IlwError(f"{name} must be {dtype}, got {t.dtype}")
-    if not t.is_contiguous():
-        raise IlwError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise IlwError(f"{name} must be contiguous")
 
 
 def _raw_stream(device) -> int:

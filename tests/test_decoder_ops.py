@@ -183,6 +183,18 @@ def test_attention_single_tokens(D, P):
         assert not want[0].any() and want[1:].any()
 
 
+@pytest.mark.parametrize("D", [32, 64, 128, 256])
+def test_attention_most_of_one_workgroup(D):
+    """16 rows of 1024 keys: the most scores that one workgroup keeps; one more
+    key is split.  The rows of one query, and those of sixteen."""
+    for heads, new, P in [(16, 1, 16), (1, 16, 64), (5, 3, 32)]:
+        for longest in (1024, 1024 + P):
+            g = rng(D, heads, longest)
+            c = make_cache(g, 3, longest // P, 1, P, D)
+            run_attention(c, heads, [new, 1, new], [longest, 3, 1024], params(D), True, 0,
+                          f"D={D} heads={heads} new={new} longest={longest}", g=g)
+
+
 @pytest.mark.parametrize("D,P,heads,hk", [(64, 16, 4, 2), (128, 64, 8, 2), (32, 32, 7, 1),
                                           (256, 128, 2, 2), (128, 16, 12, 1), (64, 256, 3, 3)])
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 70)])
