@@ -557,12 +557,12 @@ int ilw_linear_grouped(const int8_t* x, int64_t x_rows, const int32_t* rows,
  * Per-stage kernel timing (tracing; off by default).  While enabled, every
  * kernel that ilw_block_forward, ilw_encoder_forward, ilw_attention,
  * ilw_deform_attn, ilw_split_conv, ilw_patch_embed, ilw_decoder_layer,
- * ilw_cache_append, ilw_cache_attention and ilw_linear_grouped launch is bracketed by a pair of HIP events recorded on the
- * caller's stream, and the launch is attributed to one of the stages below.
- * Enabling (or disabling)
- * clears the records.  ilw_profile_read waits for the last recorded event and
- * returns, per stage, the summed kernel time in milliseconds and the number of
- * launches (arrays of n_stages entries, HOST memory).  Do not enable it while
+ * ilw_cache_append, ilw_cache_attention and ilw_linear_grouped launch is
+ * bracketed by a pair of HIP events recorded on the caller's stream (one pair
+ * for all that an ilw_cache_attention launches), and attributed to one of the
+ * stages below.  Enabling (or disabling) clears the records.  ilw_profile_read
+ * waits for the last recorded event and returns, per stage, the summed kernel
+ * time in milliseconds and the number of launches (arrays of n_stages entries, HOST memory).  Do not enable it while
  * a stream is being captured into a graph.  Launches from several threads
  * record under one lock; each launch is attributed to the stage it belongs to.
  */

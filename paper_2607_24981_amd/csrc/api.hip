@@ -10,7 +10,7 @@
 #include <string>
 #include <vector>
 
-#include "ilw_internal.h"
+#include "decoder_internal.h"
 
 using namespace ilw;
 

@@ -19,7 +19,7 @@
 // new rows of a (page, kv head), keys and values apart; the queries are groups of
 // D / 16 threads that take a head of 16-channel units each, and several heads of a
 // token one after another so that its cosines are loaded once.
-#include "ilw_internal.h"
+#include "decoder_internal.h"
 
 namespace ilw {
 namespace {

@@ -15,7 +15,7 @@
 // The sums need the exact maximum first (a weight floored at one reference is not
 // the shift of the weight floored at another), so the scores are made twice: once
 // for the maximum, once for the weights.
-#include "ilw_internal.h"
+#include "decoder_internal.h"
 
 namespace ilw {
 namespace {

@@ -11,7 +11,7 @@
 // loads of step k + 1 are in flight during the products of step k.  (Weights read
 // straight to registers where few rows use them: 34 us against 22, since a load
 // then takes 64 bytes of 16 rows where these take whole 128-byte lines.)
-#include "ilw_internal.h"
+#include "decoder_internal.h"
 
 namespace ilw {
 namespace {

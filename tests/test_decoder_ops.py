@@ -646,3 +646,24 @@ def test_workspace_of_any_content(fill):
     plain.attention(c, q, qs, [0, 2, 4], lens, params(D), 2, 3200, True, 0, want)
     same(out.view(4, heads, D), want, "attention")
     assert bool((buf[:256] == fill).all()) and bool((buf[256 + need:] == fill).all())
+
+
+def test_decoder_stages_are_timed():
+    """One entry a call, whatever it launches."""
+    g = rng(25)
+    L = Layer(g)
+    c = make_cache(g, 1, 250, L.hk, 16, L.D)
+    rows, offsets = route(g, 1, 5)
+    cache, i32 = on_device(c), lambda *v: dev(np.array(v, np.int32))
+    args = (cache, dev(g.integers(-127, 128, (1, 128)).astype(np.int8)), i32(0, 1), i32(3000),
+            i32(3001), 1, 4000, dev(rows), dev(offsets))
+    L.run(*args)
+    ilw.profile_enable(True)
+    try:
+        for _ in range(3):
+            L.run(*args)
+        got = ilw.profile_read()
+    finally:
+        ilw.profile_enable(False)
+    for stage, n in [("cache_append", 3), ("cache_attention", 3), ("gemm_grouped", 6)]:
+        assert got[stage][1] == n and 0 < got[stage][0] < 100, (stage, got[stage])
