@@ -861,7 +861,7 @@ __global__ __launch_bounds__(256) void split_scores_kernel(CacheAttnArgs a, Spli
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // (a part's tiles side by side: later parts are shorter or empty, and with a
   // tile's parts side by side some XCDs had only those: the sums of 32
-  // sequences of 2048 to 8192 keys 45.0 us so, 42.7 now)
+  // sequences of up to 8192 keys 5% slower)
   const uint32_t part_u = blockIdx.x / (uint32_t)sp.tiles, tile = blockIdx.x - part_u * (uint32_t)sp.tiles;
   const int32_t part = (int32_t)part_u;
   Few t(a, sp, tile);
@@ -898,9 +898,7 @@ __global__ __launch_bounds__(256) void split_values_kernel(CacheAttnArgs a, Spli
   __shared__ int32_t top[4][16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // (a part's tiles side by side: later parts are shorter or empty, and with a
-  // tile's parts side by side some XCDs had only those: the sums of 32
-  // sequences of 2048 to 8192 keys 45.0 us so, 42.7 now)
+  // (numbered as in the scores)
   const uint32_t part_u = blockIdx.x / (uint32_t)sp.tiles, tile = blockIdx.x - part_u * (uint32_t)sp.tiles;
   const int32_t part = (int32_t)part_u;
   Few t(a, sp, tile);
@@ -1028,7 +1026,7 @@ Plan plan(const CacheAttnArgs& a) {
   }
   // Many rows, and enough of them to fill the CUs: the kernel that shares keys
   // among the rows of a workgroup (128, or 64 of 256 channels).  16 heads of 600
-  // queries over 4696 keys each are 80 workgroups: 110 us so, 64 us split.
+  // queries over 4696 keys each are 80 workgroups: 110 us so, 59 us split.
   p.rows = rows;
   p.shared = pairs * ((rows + (a.c.D >= 256 ? 63 : 127)) / (a.c.D >= 256 ? 64 : 128));
   if (rows > 64 && p.shared >= 192 && a.max_len <= 131072) {
