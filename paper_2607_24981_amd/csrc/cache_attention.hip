@@ -600,7 +600,8 @@ struct Split {
 };
 
 // The tile of a workgroup: its sequence, kv head and rows, and the keys that some
-// of them see, end - base of them from a multiple of 64 on, in `parts` parts.
+// of them see, end - base of them from a multiple of 64 on (0 where none is seen),
+// in `parts` parts.
 struct Few {
   int32_t s, h, G, r0, rows, base, end, parts;
   __device__ __forceinline__ Few(const CacheAttnArgs& a, const Split& sp, uint32_t tile) {
@@ -615,8 +616,10 @@ struct Few {
     if (r0 >= rows) return false;
     const Span s0(a, sq, r0 / G), s1(a, sq, (min(r0 + 16, rows) - 1) / G);
     base = s0.lo & ~63;
-    end = s1.hi;
-    parts = end > s0.lo ? (end - base + sp.chunk - 1) / sp.chunk : 0;
+    // (where none is seen, none is taken: no scores of keys from base to s0.lo are
+    // written, and the one part of a tile goes on to its zeros)
+    end = s1.hi > s0.lo ? s1.hi : base;
+    parts = (end - base + sp.chunk - 1) / sp.chunk;
     return true;
   }
 };

@@ -667,3 +667,59 @@ def test_decoder_stages_are_timed():
         ilw.profile_enable(False)
     for stage, n in [("cache_append", 3), ("cache_attention", 3), ("gemm_grouped", 6)]:
         assert got[stage][1] == n and 0 < got[stage][0] < 100, (stage, got[stage])
+
+
+@pytest.mark.parametrize("fill", [0, 0x7f, 0xff])
+@pytest.mark.parametrize("D,P,heads,max_q", [(128, 64, 8, 2), (64, 16, 24, 1), (32, 128, 8, 40),
+                                             (256, 32, 16, 1)])
+@pytest.mark.parametrize("max_len,window", [(2000, 0), (2000, 1500), (1999, 1985), (1130, 1100)])
+def test_attention_split_in_one_part(D, P, heads, max_q, max_len, window, fill):
+    """Sequences enough that nothing is joined: one part writes the output, zeros
+    too where a row sees no key (none there, no page, all before the window), over
+    a workspace of exactly the size asked for that holds anything."""
+    hk, seqs = 8, 65
+    g = rng(D, P, max_len, window, fill)
+    c = scattered(g, seqs, -(-max_len // P), hk, P, D)
+    c["table"][6] = -1
+    # within, at and past max_len, and past it by about the window
+    lens = [max_len + window + max_q, max_len + window + max_q - 1, max_len + window, max_len + 1,
+            max_len, 1, max_len, 0, 4000, max_len + 63] + [int(x) for x in g.integers(0, 300, seqs - 10)]
+    new = [int(x) for x in g.integers(1, min(max_q, 3) + 1, seqs)]
+    new[0], new[1], new[2] = max_q, max_q, 1
+    T = sum(new)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    q = g.integers(-127, 128, (T, heads, D)).astype(np.int8)
+    qs = g.integers(9000, 21000, (T, heads)).astype(np.int32)
+    cache = on_device(c)
+    need = ilw.lib().ilw_cache_attention_workspace_bytes(cache.struct, seqs, max_q, max_len, heads,
+                                                         window)
+    rows = max_q * (heads // hk)
+    tiles = seqs * hk * -(-rows // 16)
+    seen = min(max_len, window + 16) if window else max_len
+    steps = -(-seen // 64) + (seen < max_len)
+    say(f"one part D={D} P={P} heads={heads} max_len={max_len} window={window} fill={fill}")
+    up = lambda n: -(-n // 256) * 256
+    assert need == up(tiles * steps * min(rows, 16) * 128) + up(tiles * 64)  # (no parts' sums)
+    buf = torch.full((need + 512,), fill, dtype=torch.uint8, device="cuda")
+    out = torch.full((T, heads * D), 77, dtype=torch.int8, device="cuda")
+    ilw.ilw_cache_attention(cache, dev(q), dev(qs), dev(cu), dev(np.array(lens, np.int32)),
+                            params(D), max_q, max_len, window=window, out=out,
+                            workspace=buf[256:256 + need].view(torch.int8))
+    want = np.full((T, heads, D), 77, np.int8)
+    plain.attention(c, q, qs, cu.tolist(), lens, params(D), max_q, max_len, True, window, want)
+    assert not window or not want[0].any()
+    same(out.view(T, heads, D), want, "attention")
+    assert bool((buf[:256] == fill).all()) and bool((buf[256 + need:] == fill).all())
+
+
+def test_attention_rows_past_max_len_and_window():
+    """The same lengths by the kernel of many rows and by one workgroup a tile."""
+    D, P, hk, window = 64, 32, 4, 45
+    for seqs, max_q, max_len in [(64, 70, 200), (3, 2, 200)]:
+        g = rng(max_q, 7)
+        c = scattered(g, seqs, -(-max_len // P), hk, P, D)
+        lens = [max_len + window + max_q, max_len + window, max_len + 1] + [int(x) for x in g.integers(
+            0, 60, seqs - 3)]
+        want = run_attention(c, hk, [max_q, 1] + [1] * (seqs - 2), lens, params(D), True, window,
+                             f"past max_len and window, {seqs} sequences", g=g, max_len=max_len)
+        assert not want[0].any()
