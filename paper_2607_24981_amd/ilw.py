@@ -638,26 +638,38 @@ class KVCache:
     """A paged int8 cache: pools k and v int8 [n_pages, kv_heads, page_size,
     head_dim] (v's order within a page: see include/ilw.h), scales int32
     [n_pages, kv_heads] and page_table int32 [sequences, max_pages].  The
-    tensors stay the caller's; appending changes them in place."""
+    tensors stay the caller's; appending changes them in place.  page_table may
+    be set to another tensor, of other sequences too; everything else stays what
+    the cache was made with, since calls go by the addresses in `struct`."""
 
     def __init__(self, k, v, k_scale, v_scale, page_table):
-        self.device = dev = _device(k, "k")
+        dev = _device(k, "k")
         if k.dim() != 4 or v.shape != k.shape:
             raise IlwError("k and v must be [n_pages, kv_heads, page_size, head_dim], got "
                            f"{tuple(k.shape)} and {tuple(v.shape)}")
         n, h, p, d = k.shape
         _shape(k_scale, (n, h), "k_scale")
         _shape(v_scale, (n, h), "v_scale")
-        if page_table.dim() != 2:
-            raise IlwError("page_table must be [sequences, max_pages]")
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.__dict__.update(
+            device=dev, k=k, v=v, k_scale=k_scale, v_scale=v_scale, kv_heads=h, page_size=p,
+            head_dim=d, _pools=(_at(k, torch.int8, "k", dev), _at(v, torch.int8, "v", dev),
+                                _at(k_scale, torch.int32, "k_scale", dev),
+                                _at(v_scale, torch.int32, "v_scale", dev)))
         self.page_table = page_table
-        self.seqs, pages = page_table.shape
-        self.kv_heads, self.page_size, self.head_dim = h, p, d
-        self.struct = KVCacheStruct(
-            _at(k, torch.int8, "k", dev), _at(v, torch.int8, "v", dev),
-            _at(k_scale, torch.int32, "k_scale", dev), _at(v_scale, torch.int32, "v_scale", dev),
-            _at(page_table, torch.int32, "page_table", dev), n, p, pages, h, d)
+
+    def __setattr__(self, name, value):
+        if name != "page_table":
+            raise IlwError(f"{name} of a cache stays as it was made: make another KVCache")
+        if value.dim() != 2:
+            raise IlwError("page_table must be [sequences, max_pages]")
+        at = _at(value, torch.int32, "page_table", self.device)
+        seqs, pages = value.shape
+        struct = KVCacheStruct(*self._pools, at, self.k.shape[0], self.page_size, pages,
+                               self.kv_heads, self.head_dim)
+        self.__dict__.update(page_table=value, seqs=seqs, struct=struct)
+
+    def __delattr__(self, name):
+        raise IlwError(f"{name} of a cache stays as it was made")
 
     @classmethod
     def empty(cls, n_pages, kv_heads, page_size, head_dim, page_table):

@@ -164,6 +164,45 @@ def test_binding_refuses_host_tensors_and_shapes():
                                z(3, dtype=torch.int32), None, s, s)
 
 
+def host_cache(monkeypatch, seqs=2, max_pages=3):
+    """A cache of host tensors, which no call is given."""
+    monkeypatch.setattr(ilw, "_device", lambda t, name: -1)
+    z = torch.zeros
+    k, v = (z(4, 2, 16, 64, dtype=torch.int8) for _ in range(2))
+    ks, vs = (z(4, 2, dtype=torch.int32) for _ in range(2))
+    return ilw.KVCache(k, v, ks, vs, z(seqs, max_pages, dtype=torch.int32))
+
+
+def test_cache_follows_its_page_table(monkeypatch):
+    """A page table set later is the one that calls get, and its sequences."""
+    cache = host_cache(monkeypatch)
+    fixed = {n: getattr(cache.struct, n) for n, _ in ilw.KVCacheStruct._fields_}
+    table = torch.ones(5, 7, dtype=torch.int32)
+    cache.page_table = table
+    fixed.update(page_table=table.data_ptr(), max_pages=7)
+    assert {n: getattr(cache.struct, n) for n, _ in ilw.KVCacheStruct._fields_} == fixed
+    assert cache.page_table is table and cache.seqs == 5
+    for bad in [table[0], table.long(), torch.ones(5, 8, dtype=torch.int32)[:, :7], table.t()]:
+        with pytest.raises(ilw.IlwError):
+            cache.page_table = bad
+        assert cache.page_table is table and cache.struct.page_table == table.data_ptr()
+
+
+def test_cache_keeps_what_it_was_made_with(monkeypatch):
+    """Nothing else changes beside the addresses that calls go by."""
+    cache = host_cache(monkeypatch)
+    for name in ["k", "v", "k_scale", "v_scale", "struct", "seqs", "kv_heads", "page_size",
+                 "head_dim", "device"]:
+        was = getattr(cache, name)
+        with pytest.raises(ilw.IlwError, match=name):
+            setattr(cache, name, torch.zeros(4, 2, 16, 64, dtype=torch.int8))
+        with pytest.raises(ilw.IlwError):
+            delattr(cache, name)
+        assert getattr(cache, name) is was
+    for name in ("k", "v", "k_scale", "v_scale"):
+        assert getattr(cache.struct, name) == getattr(cache, name).data_ptr()
+
+
 # ------------------------------------------- the plain forms that the GPU meets
 @pytest.mark.parametrize("P,D", [(16, 32), (32, 64), (64, 128), (128, 256), (256, 32)])
 def test_value_order_is_a_permutation(P, D):

@@ -723,3 +723,31 @@ def test_attention_rows_past_max_len_and_window():
         want = run_attention(c, hk, [max_q, 1] + [1] * (seqs - 2), lens, params(D), True, window,
                              f"past max_len and window, {seqs} sequences", g=g, max_len=max_len)
         assert not want[0].any()
+
+
+def test_another_page_table():
+    """The same pools under a table that is set after a first call: other pages, and
+    then another number of sequences."""
+    D, P, heads, hk = 64, 16, 4, 2
+    g = rng(26)
+    c = make_cache(g, 3, 6, hk, P, D)
+    cache, first = on_device(c), c["table"]
+    rope = rope_of(6 * P, D)
+    for table in (first, first[::-1].copy(), first[1:, :5].copy(), first):
+        seqs = len(table)
+        c["table"] = table
+        cache.page_table = dev(table)
+        past, new = np.array([20, 0, 40], np.int32)[:seqs], np.array([2, 3, 1], np.int32)[:seqs]
+        cu, T = np.concatenate([[0], np.cumsum(new)]).astype(np.int32), int(new.sum())
+        qkv = g.integers(-127, 128, (T, (heads + 2 * hk) * D)).astype(np.int8)
+        say(f"table of {seqs} sequences")
+        q, qs = ilw.ilw_cache_append(cache, dev(qkv), heads, dev(cu), dev(past), 3, rope=dev(rope))
+        out = ilw.ilw_cache_attention(cache, q, qs, dev(cu), dev(past + new), params(D), 3, 80)
+        want_q, want_s = np.zeros((T, heads, D), np.int8), np.zeros((T, heads), np.int32)
+        plain.append(c, qkv, heads, cu.tolist(), past.tolist(), 3, rope, False, want_q, want_s)
+        want = np.zeros_like(want_q)
+        plain.attention(c, want_q, want_s, cu.tolist(), (past + new).tolist(), params(D), 3, 80, True,
+                        0, want)
+        same(q, want_q, "q")
+        same_cache(cache, c, "cache")
+        same(out.view(T, heads, D), want, "attention")
