@@ -238,6 +238,13 @@ struct Digits {
   }
 };
 
+// The sum of up to 2^17 products of low digits and values from its int32, which has
+// wrapped where every one of 2^17 products is (-128)^2: 2^31 stands there as -2^31,
+// which no sum is (the least is 2^17 * -128 * 127).
+__device__ __forceinline__ int64_t low_sum(int32_t s) {
+  return (int64_t)(int32_t)((uint32_t)s - 1) + 1;
+}
+
 // Sum over the 4 lanes of a row.
 __device__ __forceinline__ uint64_t sum_over_lanes(uint32_t v) {
   uint64_t l = (uint64_t)v + (uint32_t)__shfl_xor((int)v, 16, 64);
@@ -581,7 +588,7 @@ void cache_rows_kernel(CacheAttnArgs a, uint32_t tiles) {
       int32_t v[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        v[r] = nm.out((int64_t)oh[g][f][r] * 256 + ol[g][f][r], a);
+        v[r] = nm.out((int64_t)oh[g][f][r] * 256 + low_sum(ol[g][f][r]), a);
       *(uint32_t*)(a.out + R.at[f] * D + g * 16 + (lane >> 4) * 4) = pack4(v[0], v[1], v[2], v[3]);
     }
   }

@@ -751,3 +751,23 @@ def test_another_page_table():
         same(q, want_q, "q")
         same_cache(cache, c, "cache")
         same(out.view(T, heads, D), want, "attention")
+
+
+@pytest.mark.parametrize("code", [-128, 127])
+@pytest.mark.parametrize("D,P", [(32, 256), (128, 16)])
+def test_attention_lowest_codes_of_a_long_prompt(D, P, code):
+    """131072 keys of one weight, every value -128 (which appending never writes)
+    under a scale whose low digit is -128: 2^31, one more than an int32 sum holds;
+    and the lowest sum that there is, of 127."""
+    max_len, hk, seqs = 131072, 4, 48
+    g = rng(D, code + 128)
+    c = scattered(g, seqs, max_len // P, hk, P, D)
+    c["v"][:] = code
+    c["v_scale"][:] = 72 * 256 + 128
+    # (below saturation; a wrong sum of low digits moves it by two codes)
+    p = {"score_mult": 0, "score_shift": 40, "out_mult": 107 << 24, "out_shift": 47}
+    new = [2] + [1] * (seqs - 1)
+    lens = [max_len, 40] + [int(x) for x in g.integers(0, 90, seqs - 2)]
+    want = run_attention(c, hk, new, lens, p, False, 0, f"lowest codes D={D} code={code}", g=g,
+                         max_q=66)
+    assert (want[0] == want[0, 0, 0]).all() and 100 < abs(int(want[0, 0, 0])) < 127
