@@ -56,8 +56,8 @@ def named(kernels, name):
 
 
 @pytest.mark.parametrize("name,instances", [
-    ("append_kernel", 2), ("cache_rows_kernel", 24), ("split_scores_kernel", 12),
-    ("split_values_kernel", 12), ("split_join_kernel", 4), ("grouped_kernel", 8)])
+    ("append_kernel", 2), ("cache_rows_kernel", 24), ("cache_few_kernel", 12),
+    ("split_scores_kernel", 12), ("split_values_kernel", 12), ("split_join_kernel", 4), ("grouped_kernel", 8)])
 def test_no_private_memory(kernels, name, instances):
     """No spills, and no array that is indexed in memory."""
     found = named(kernels, name)
@@ -65,3 +65,10 @@ def test_no_private_memory(kernels, name, instances):
     bad = {k: (v[".private_segment_fixed_size"], v[".vgpr_spill_count"]) for k, v in found.items()
            if v[".private_segment_fixed_size"] or v[".vgpr_spill_count"]}
     assert not bad
+
+
+@pytest.mark.parametrize("name", ["cache_rows_kernel", "cache_few_kernel", "split_scores_kernel",
+                                  "split_values_kernel"])
+def test_two_waves_a_simd(kernels, name):
+    """256 registers a lane at most, accumulation registers among them."""
+    assert max(v[".vgpr_count"] for v in named(kernels, name).values()) <= 256
