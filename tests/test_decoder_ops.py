@@ -771,3 +771,20 @@ def test_attention_lowest_codes_of_a_long_prompt(D, P, code):
     want = run_attention(c, hk, new, lens, p, False, 0, f"lowest codes D={D} code={code}", g=g,
                          max_q=66)
     assert (want[0] == want[0, 0, 0]).all() and 100 < abs(int(want[0, 0, 0])) < 127
+
+
+@pytest.mark.parametrize("K", [144, 272, 400])
+def test_grouped_largest_tile_with_a_tail(K):
+    """256 x 256 tiles whose last step is 16 inputs after whole ones: loads straight
+    to LDS, then stores, into the same two buffers."""
+    counts, N = [1900, 0, 201], 4224
+    assert sum(counts) >= 192 * len(counts) and sum(counts) * N > 128 * 65536
+    run_grouped(rng(N, K), counts, N, K, x_rows=300, pad=1)
+
+
+@pytest.mark.parametrize("counts,N", [([70, 130, 65], 6032), ([3, 0, 9, 16] * 33, 1024),
+                                      ([40, 7], 144)])
+def test_grouped_other_tiles_with_a_tail(counts, N):
+    """The same of the other three tiles."""
+    for K in (272, 208):
+        run_grouped(rng(N, K), counts, N, K, x_rows=90, pad=1)
