@@ -650,23 +650,22 @@ class KVCache:
         n, h, p, d = k.shape
         _shape(k_scale, (n, h), "k_scale")
         _shape(v_scale, (n, h), "v_scale")
-        self.__dict__.update(
-            device=dev, k=k, v=v, k_scale=k_scale, v_scale=v_scale, kv_heads=h, page_size=p,
-            head_dim=d, _pools=(_at(k, torch.int8, "k", dev), _at(v, torch.int8, "v", dev),
-                                _at(k_scale, torch.int32, "k_scale", dev),
-                                _at(v_scale, torch.int32, "v_scale", dev)))
-        self.page_table = page_table
+        if page_table.dim() != 2:
+            raise IlwError("page_table must be [sequences, max_pages]")
+        seqs, pages = page_table.shape
+        at = self.__dict__  # (past __setattr__)
+        at["device"], at["k"], at["v"], at["k_scale"], at["v_scale"] = dev, k, v, k_scale, v_scale
+        at["kv_heads"], at["page_size"], at["head_dim"] = h, p, d
+        at["page_table"], at["seqs"] = page_table, seqs
+        at["struct"] = KVCacheStruct(
+            _at(k, torch.int8, "k", dev), _at(v, torch.int8, "v", dev),
+            _at(k_scale, torch.int32, "k_scale", dev), _at(v_scale, torch.int32, "v_scale", dev),
+            _at(page_table, torch.int32, "page_table", dev), n, p, pages, h, d)
 
     def __setattr__(self, name, value):
         if name != "page_table":
             raise IlwError(f"{name} of a cache stays as it was made: make another KVCache")
-        if value.dim() != 2:
-            raise IlwError("page_table must be [sequences, max_pages]")
-        at = _at(value, torch.int32, "page_table", self.device)
-        seqs, pages = value.shape
-        struct = KVCacheStruct(*self._pools, at, self.k.shape[0], self.page_size, pages,
-                               self.kv_heads, self.head_dim)
-        self.__dict__.update(page_table=value, seqs=seqs, struct=struct)
+        self.__dict__.update(KVCache(self.k, self.v, self.k_scale, self.v_scale, value).__dict__)
 
     def __delattr__(self, name):
         raise IlwError(f"{name} of a cache stays as it was made")
