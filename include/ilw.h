@@ -544,7 +544,8 @@ int ilw_cache_attention(const ilw_kv_cache* cache, const int8_t* q, const int32_
  *            outside [offsets[0], offsets[experts]) are left as they are
  *   w int8 [experts, N, K], b int32 [experts, N] or NULL, y int8 [M, N]
  *   rq       n = 1 (one factor for all) or experts * N
- * N and K multiples of 16, K <= 131072, experts in [1, 1024], (M/64 + experts) *
+ * N and K multiples of 16, K <= 131072 (the sums are int32: at 131072 not every
+ * product may be of -128 and -128), experts in [1, 1024], (M/64 + experts) *
  * (N/128 + 1) < 2^22 (whole quotients); x and w 16-byte aligned, y 4-byte
  * aligned and not aliasing x.  M == 0 is a no-op.
  */

@@ -12,8 +12,8 @@
 // the product's high word: a shift, a 64-bit multiply-add and the byte permutes
 // of the packing.
 //
-// Bound: one round trip through memory after the other (a few tokens: 4 us of one
-// sequence, 5 of 64), bytes and the registers that keep them in flight (a prompt
+// Bound: one round trip through memory after the other (a few tokens: 3.8 us of one
+// sequence, 5.3 of 64), bytes and the registers that keep them in flight (a prompt
 // of 16384 tokens, 32 + 8 heads of 128: 41 us for the 31 that its 144 MB take to
 // copy).  A team of threads, a wave for a few tokens and two for many, takes the
 // new rows of a (page, kv head), keys and values apart; the queries are groups of
@@ -178,9 +178,9 @@ __device__ __forceinline__ bool page_of(const AppendArgs& a, int32_t s, const Pa
 
 // Two passes over the units, for the scale and with it, in opposite directions:
 // the unit held last is used first, and with one unit a thread (a few tokens)
-// nothing is read twice.  (Holding 2 or 4 units saves no time: 43 and 59
-// us a prompt against 42, at 117 and 128 registers against 70; nor does holding
-// the cosines: 48, at 90.)
+// nothing is read twice.  (Holding 2 or 4 units saves no time: 43 and 59 us a prompt
+// against 42, nor does holding the cosines: 48.  Both cost registers, of which the
+// kernel takes 85, five waves a SIMD.)
 template <int TS>
 __device__ void append_keys(const AppendArgs& a, const Rows& r, int32_t s, const Part& p,
                             int32_t h, int tid, uint32_t* lds) {

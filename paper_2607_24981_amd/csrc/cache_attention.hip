@@ -1062,9 +1062,12 @@ Plan plan(const CacheAttnArgs& a) {
     return p;
   }
   p.way = SPLIT;
-  // Parts enough for two workgroups a CU, of at least 512 keys.  (131072 keys of 8
-  // kv heads in 512, 1024 and 2048 parts: 30, 32 and 36 us for the scores, 29, 34
-  // and 42 for the sums: a part costs its start.)
+  // Parts enough for two workgroups a CU, of at least 512 keys, if every sequence had
+  // max_len of them (what they have is on the device).  (One sequence of 131072 keys
+  // and 8 kv heads in 512, 1024 and 2048 parts: 30, 32 and 36 us for the scores, 29,
+  // 34 and 42 for the sums: a part costs its start.  Of ragged sequences the longest
+  // sets the time: 32 of 2227 to 8192 keys, 5148 on average, take 1.6 times their
+  // bytes' time, and finer parts were not measured on them.)
   int64_t chunk = (seen * p.tiles + 511) / 512;
   chunk = (chunk + 255) / 256 * 256;
   if (chunk < 512) chunk = 512;

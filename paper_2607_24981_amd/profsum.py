@@ -91,7 +91,8 @@ def kernels(args):
                       f"{k}  {grid}")
     if shapes:
         print("# launch shape of the first dispatch: grid (threads), workgroup, LDS bytes, "
-              "VGPR, AGPR, scratch")
+              "scratch; vgpr and agpr as the profiler reports them (on gfx950 vgpr is half of "
+              "what is allocated where there are no agprs)")
         for k, (gx, gy, gz, wx, lds, v, a, sc) in shapes.items():
             print(f"#   {k}: grid {gx}x{gy}x{gz} wg {wx} lds {lds} vgpr {v} agpr {a} "
                   f"scratch {sc}")
