@@ -42,7 +42,7 @@
 extern "C" {
 #endif
 
-#define ILW_ABI_VERSION 10
+#define ILW_ABI_VERSION 11
 
 typedef enum {
   ILW_OK = 0,
@@ -555,13 +555,152 @@ int ilw_linear_grouped(const int8_t* x, int64_t x_rows, const int32_t* rows,
                        int32_t K, void* stream);
 
 /* ------------------------------------------------------------------------
+ * int16 rows to int8 codes with a scale for each row (token): activations whose
+ * range is known only when they are there, for ilw_linear_scaled.
+ *   x      int16 [M, K], rows ld values apart (ld >= K, a multiple of 8)
+ *   y      int8 [M, K], scale int32 [M]
+ * With A the largest magnitude of a row (-32768 counts as 32768):
+ *   scale = max(1, ceil(2^14 A / 127));  y = floor((2^15 x + scale) / (2 scale))
+ * in [-127, 127]: a code c stands for c * scale / 2^14 in units of x, as in the
+ * paged cache above.  K a multiple of 16 in [16, 2^20]; x and y 16-byte aligned;
+ * M == 0 is a no-op.  One launch; no workspace.  Calls whose M and K need more than
+ * a launch's 2^32 threads are refused with ILW_E_UNSUPPORTED.
+ */
+int ilw_quantize_rows(const int16_t* x, int64_t ld, int8_t* y, int32_t* scale, int64_t M,
+                      int32_t K, void* stream);
+
+/* Integer linear layer with a scale for each token and a factor for each channel
+ * (Sec. 3.2.1's linear with scales that are not folded beforehand), dense or over
+ * rows sorted by expert:
+ *   y[m][n] = sat(x_scale[r]/2^14 * mult[e][n]/2^shift[e][n] * sum_k x[r][k] w[e][n][k]
+ *                 + b[e][n]/16), to the nearest, halves up
+ *   x        int8 [x_rows, K], x_scale int32 [x_rows] in [1, 2^31) (others count as a
+ *            factor of 0);  r = m, or rows[m] where rows is not NULL (DEVICE int32
+ *            [M]; an r outside [0, x_rows) reads a row of zeros)
+ *   offsets  NULL: one expert (experts == 1) has every row.  Else DEVICE int32
+ *            [experts + 1], not decreasing, in [0, M]: expert e has rows offsets[e]
+ *            .. offsets[e+1] - 1, and rows of y outside [offsets[0],
+ *            offsets[experts]) are left as they are
+ *   w        int8 [experts, N, K]
+ *   b        int32 [experts, N] in sixteenths of y's unit, limited to +-2^24, or NULL
+ *   rq       mult in [0, 2^31) (a negative one counts as 0), shift in [1, 62]; n = 1
+ *            (one factor for all) or experts * N
+ *   y        int16 (y_bits 16, sat to +-32767) or int8 (y_bits 8, +-127) [M, N]
+ * In integers, with X = x_scale 2^z in [2^31, 2^32), Y = mult 2^u in [2^30, 2^31):
+ *   F = floor(X Y / 2^32);  q = shift + z + u - 18
+ *   y = sat(floor((floor(acc F / 2^max(q - 4, 0)) + b + 8) / 16))
+ * so that a factor keeps 29 bits or more, whatever the two scales are.
+ * N and K multiples of 16, K <= 131072 (the sums are int32: at 131072 not every
+ * product may be of -128 and -128), experts in [1, 1024], (M/64 + experts) *
+ * (N/128 + 1) < 2^22 (whole quotients); x and w 16-byte aligned, y 4-byte aligned
+ * and not aliasing x.  M == 0 is a no-op.  No workspace.
+ */
+int ilw_linear_scaled(const int8_t* x, int64_t x_rows, const int32_t* x_scale,
+                      const int32_t* rows, const int32_t* offsets, const int8_t* w,
+                      const int32_t* b, ilw_dyadic rq, void* y, int32_t y_bits, int64_t M,
+                      int32_t experts, int32_t N, int32_t K, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Routing of tokens to experts, and the experts' rows back to tokens.
+ *
+ * ilw_route takes int16 scores [tokens, experts] in 1/64 octave (rows ld values
+ * apart, ld >= experts; the router's ilw_linear_scaled folds log2(e) and 64 in its
+ * factors).  -32768, which ilw_linear_scaled never writes, is an expert that the
+ * token may not have; a token with no other score (padding) gets none.  With
+ *   e(a) = E[a % 64] >> (a / 64),  E[f] = 2^(30 - f/64) to the nearest
+ *   R(D) = floor((2^62 - 1) / D)
+ * a score s has the probability, in 2^-30,
+ *   softmax  w = e(max s - s), L = sum w, d = bit length of L, - 31:
+ *            p = (w R(L >> d)) >> (32 + d)
+ *   sigmoid  t = e(|s|):  p = ((s < 0 ? t : 2^30) R(2^30 + t)) >> 32
+ * and its choice goes by p + bias (bias int32 [experts] in 2^-30, limited to +-2^30,
+ * or NULL), ties to the lower index.  groups > 1: the experts are `groups` runs of
+ * experts / groups neighbours, and only those of the top_groups runs with the
+ * largest sums of their group_best (1 or 2) best choices can be had.  The top_k best
+ * are chosen, in that order.  Their weights are r = p, or with renormalize = 1, W
+ * being the sum of the chosen p and n its bit length,
+ *   r = (p R(W 2^(31-n))) >> (n + 1)   (W 2^(31-n) rounded down; 0 where W is 0)
+ *   weight = min((r weight_mult + 2^(weight_shift-1)) >> weight_shift, 2^31 - 1)
+ * (weight_mult / 2^weight_shift = 2^-14 gives weights in 2^-16).
+ *   expert, weight  int32 [tokens, top_k]; -1 and 0 where a token gets fewer
+ *   offsets  int32 [experts + 1], rows int32 [tokens * top_k], slot int32 [tokens,
+ *            top_k]: the choices sorted by expert, then by token.  Row i of expert
+ *            e, offsets[e] <= i < offsets[e+1], is of token rows[i], and choice j of
+ *            token t is row slot[t][j] (-1: none); rows from offsets[experts] on are
+ *            -1.  They are what ilw_linear_grouped, ilw_linear_scaled and ilw_combine
+ *            take.
+ * experts in [1, 1024], a multiple of groups; groups in [1, 64], top_groups in [1,
+ * groups]; top_k in [1, min(32, experts)]; weight_mult in [0, 2^31), weight_shift in
+ * [1, 62]; tokens * top_k < 2^31.  At most two launches.  The workspace may hold
+ * anything; calls that may run at the same time need one each.
+ */
+typedef struct {
+  int32_t top_k, groups, top_groups, group_best;
+  int32_t sigmoid, renormalize;
+  int32_t weight_mult, weight_shift;
+} ilw_route_params;
+
+size_t ilw_route_workspace_bytes(int32_t tokens, int32_t experts);
+int ilw_route(const int16_t* logits, int64_t ld, const int32_t* bias, int32_t* expert,
+              int32_t* weight, int32_t* offsets, int32_t* rows, int32_t* slot, int32_t tokens,
+              int32_t experts, const ilw_route_params* rp, void* workspace,
+              size_t workspace_bytes, void* stream);
+
+/* The experts' rows weighted and summed back to tokens, with a skip (the residual
+ * form of ilw_residual_add):
+ *   U = (sum_j weight[t][j] v[slot[t][j]][n] + 2^7) >> 8, limited to +-(2^31 - 1)
+ *   y[t][n] = sat(floor((U mult_a + skip[t][n] mult_b + 2^(shift-1)) / 2^shift))
+ *   v        int8 or int16 (bits 8 or 16) [v_rows, N]; a slot outside [0, v_rows)
+ *            adds nothing
+ *   slot, weight  int32 [tokens, top_k], any weights
+ *   skip     as v, [tokens, N], or NULL;  y as v, [tokens, N], may alias skip, not v
+ * N a multiple of 16, below 2^24; top_k in [1, 32]; mult_a, mult_b any int32 except
+ * INT32_MIN, shift in [1, 62]; v, skip and y 16-byte aligned.  tokens == 0 is a
+ * no-op.  One launch; no workspace.  Calls whose tokens and N need more than a
+ * launch's 2^32 threads are refused with ILW_E_UNSUPPORTED.
+ */
+int ilw_combine(const void* v, int32_t bits, int64_t v_rows, const int32_t* slot,
+                const int32_t* weight, const void* skip, int32_t mult_a, int32_t mult_b,
+                int32_t shift, void* y, int64_t tokens, int32_t top_k, int32_t N, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Log probabilities of given tokens, the entropy and the best alternatives of rows
+ * of int16 vocabulary scores s in 1/64 octave (-32768: a token that may not be had).
+ *   logits   int16 [rows, vocab], rows ld values apart (ld >= vocab, 2-byte aligned)
+ *   given    int32 [rows, n_given];  given_lp int32 [rows, n_given]
+ *   entropy  int32 [rows]
+ *   top, top_lp  int32 [rows, n_top]: the best scores in order, ties to the lower
+ *            index, and their log probabilities
+ * log2 probabilities and the entropy in bits, both in 2^-16; with e as above, a =
+ * max s - s over the scores that can be had:
+ *   L = sum e(a);  lg = log2(L / 2^30): with n the bit length of L and y = L >> (n -
+ *       31), 16 times y = y y >> 30, a bit of the fraction y >= 2^31, then halved if
+ *       so; after n - 31 before the point
+ *   log2 p = 1024 (s - max s) - lg
+ *   entropy = lg + floor(1024 sum(e(a) a) / L)
+ * A token that may not be had, or outside [0, vocab), has INT32_MIN.  Where fewer
+ * than n_top can be had the rest of top is -1, of top_lp INT32_MIN; a row in which
+ * none can be had has entropy 0.
+ * vocab in [1, 2^20], n_given and n_top in [0, 64].  rows == 0 is a no-op.  At most
+ * three launches.  The workspace (its size follows from rows, vocab and n_top and may
+ * be 0) may hold anything; calls that may run at the same time need one each.  Calls
+ * that need more than a launch's 2^32 threads are refused with ILW_E_UNSUPPORTED.
+ */
+size_t ilw_log_probs_workspace_bytes(int64_t rows, int32_t vocab, int32_t n_top);
+int ilw_log_probs(const int16_t* logits, int64_t ld, const int32_t* given, int32_t n_given,
+                  int32_t* given_lp, int32_t* entropy, int32_t* top, int32_t* top_lp,
+                  int64_t rows, int32_t vocab, int32_t n_top, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Per-stage kernel timing (tracing; off by default).  While enabled, every
  * kernel that ilw_block_forward, ilw_encoder_forward, ilw_attention,
  * ilw_deform_attn, ilw_split_conv, ilw_patch_embed, ilw_decoder_layer,
- * ilw_cache_append, ilw_cache_attention and ilw_linear_grouped launch is
+ * ilw_cache_append, ilw_cache_attention, ilw_linear_grouped, ilw_quantize_rows,
+ * ilw_linear_scaled, ilw_route, ilw_combine and ilw_log_probs launch is
  * bracketed by a pair of HIP events recorded on the caller's stream (one pair
- * for all that an ilw_cache_attention launches), and attributed to one of the
- * stages below.  Enabling (or disabling) clears the records.  ilw_profile_read
+ * for all that an ilw_cache_attention, ilw_route or ilw_log_probs launches), and
+ * attributed to one of the stages below.  Enabling (or disabling) clears the records.  ilw_profile_read
  * waits for the last recorded event and returns, per stage, the summed kernel
  * time in milliseconds and the number of launches (arrays of n_stages entries, HOST memory).  Do not enable it while
  * a stream is being captured into a graph.  Launches from several threads
@@ -585,7 +724,12 @@ typedef enum {
   ILW_STAGE_CACHE_APPEND = 13, /* rotation and append to the paged cache    */
   ILW_STAGE_CACHE_ATTENTION = 14, /* attention over the paged cache         */
   ILW_STAGE_GEMM_GROUPED = 15, /* linears grouped by expert                 */
-  ILW_NUM_STAGES = 16
+  ILW_STAGE_QUANTIZE = 16,   /* rows quantized with a scale each            */
+  ILW_STAGE_GEMM_SCALED = 17, /* linears with token and channel scales      */
+  ILW_STAGE_ROUTE = 18,      /* routing to experts                          */
+  ILW_STAGE_COMBINE = 19,    /* experts' rows back to tokens                */
+  ILW_STAGE_LOG_PROBS = 20,  /* log probabilities                           */
+  ILW_NUM_STAGES = 21
 } ilw_stage;
 
 int ilw_profile_enable(int enable);

@@ -16,7 +16,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 SO = os.path.join(HERE, "libilw.so")
 SOURCES = ["api.hip", "gemm.hip", "ln_gemm.hip", "tail384.hip", "attention.hip", "rowops.hip",
            "deform.hip", "block_tail.hip", "split_conv.hip", "cache_append.hip",
-           "cache_attention.hip", "grouped.hip"]
+           "cache_attention.hip", "grouped.hip", "quantize_rows.hip", "linear_scaled.hip",
+           "experts.hip", "log_probs.hip"]
 ARCH = "gfx950"
 
 

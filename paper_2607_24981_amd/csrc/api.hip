@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "decoder_internal.h"
+#include "step_internal.h"
 
 using namespace ilw;
 
@@ -133,6 +134,40 @@ int check_shift(int32_t s, const char* name) {
 
 int check_mult(int32_t m, const char* name) {
   REQUIRE(m != INT32_MIN, ILW_E_PARAM, "%s must not be INT32_MIN", name);
+  return ILW_OK;
+}
+
+// Sizes of a linear over rows that may be sorted by expert.
+int check_expert_linear(int64_t M, int64_t x_rows, const int32_t* rows, int32_t experts, int32_t N,
+                        int32_t K) {
+  REQUIRE(M >= 0 && x_rows >= 0 && N >= 16 && K >= 16, ILW_E_SHAPE,
+          "M=%lld x_rows=%lld N=%d K=%d invalid", (long long)M, (long long)x_rows, N, K);
+  REQUIRE(experts >= 1 && experts <= 1024, ILW_E_SHAPE, "experts = %d must be in [1, 1024]",
+          experts);
+  REQUIRE(N % 16 == 0 && K % 16 == 0, ILW_E_SHAPE, "N=%d and K=%d must be multiples of 16", N, K);
+  REQUIRE(K <= 131072, ILW_E_UNSUPPORTED, "K=%d: the int32 accumulator needs K <= 131072", K);
+  REQUIRE((int64_t)experts * N < ((int64_t)1 << 31), ILW_E_UNSUPPORTED,
+          "experts * N = %lld must be below 2^31", (long long)experts * N);
+  REQUIRE(M < ((int64_t)1 << 31) && x_rows < ((int64_t)1 << 31), ILW_E_UNSUPPORTED,
+          "M=%lld and x_rows=%lld must be below 2^31", (long long)M, (long long)x_rows);
+  // (the grid of every tile size then stays under 2^32 threads)
+  REQUIRE((M / 64 + experts) * (N / 128 + 1) < (int64_t)1 << 22, ILW_E_UNSUPPORTED,
+          "(M / 64 + experts) * (N / 128 + 1) = %lld must be below 2^22",
+          (long long)((M / 64 + experts) * (N / 128 + 1)));
+  REQUIRE(rows || x_rows >= M, ILW_E_SHAPE, "x has %lld rows, %lld needed", (long long)x_rows,
+          (long long)M);
+  return ILW_OK;
+}
+
+int check_log_probs(int64_t rows, int32_t vocab, int32_t n_top) {
+  REQUIRE(rows >= 0, ILW_E_SHAPE, "rows = %lld must be >= 0", (long long)rows);
+  REQUIRE(vocab >= 1 && vocab <= 1 << 20, ILW_E_SHAPE, "vocab = %d must be in [1, 2^20]", vocab);
+  REQUIRE(n_top >= 0 && n_top <= 64, ILW_E_SHAPE, "n_top = %d must be in [0, 64]", n_top);
+  LogProbArgs a = {};
+  a.rows = rows;
+  a.V = vocab;
+  REQUIRE(log_probs_fits(a), ILW_E_UNSUPPORTED, "rows = %lld of vocab = %d: too many for a launch",
+          (long long)rows, vocab);
   return ILW_OK;
 }
 
@@ -1568,22 +1603,8 @@ int ilw_linear_grouped(const int8_t* x, int64_t x_rows, const int32_t* rows,
                        const int32_t* offsets, const int8_t* w, const int32_t* b,
                        ilw_dyadic rq, int8_t* y, int64_t M, int32_t experts, int32_t N,
                        int32_t K, void* stream) {
-  REQUIRE(M >= 0 && x_rows >= 0 && N >= 16 && K >= 16, ILW_E_SHAPE,
-          "M=%lld x_rows=%lld N=%d K=%d invalid", (long long)M, (long long)x_rows, N, K);
-  REQUIRE(experts >= 1 && experts <= 1024, ILW_E_SHAPE, "experts = %d must be in [1, 1024]",
-          experts);
-  REQUIRE(N % 16 == 0 && K % 16 == 0, ILW_E_SHAPE, "N=%d and K=%d must be multiples of 16", N, K);
-  REQUIRE(K <= 131072, ILW_E_UNSUPPORTED, "K=%d: the int32 accumulator needs K <= 131072", K);
-  REQUIRE((int64_t)experts * N < ((int64_t)1 << 31), ILW_E_UNSUPPORTED,
-          "experts * N = %lld must be below 2^31", (long long)experts * N);
-  REQUIRE(M < ((int64_t)1 << 31) && x_rows < ((int64_t)1 << 31), ILW_E_UNSUPPORTED,
-          "M=%lld and x_rows=%lld must be below 2^31", (long long)M, (long long)x_rows);
-  // (the grid of every tile size then stays under 2^32 threads)
-  REQUIRE((M / 64 + experts) * (N / 128 + 1) < (int64_t)1 << 22, ILW_E_UNSUPPORTED,
-          "(M / 64 + experts) * (N / 128 + 1) = %lld must be below 2^22",
-          (long long)((M / 64 + experts) * (N / 128 + 1)));
-  REQUIRE(rows || x_rows >= M, ILW_E_SHAPE, "x has %lld rows, %lld needed", (long long)x_rows,
-          (long long)M);
+  int e;
+  if ((e = check_expert_linear(M, x_rows, rows, experts, N, K))) return e;
   if (M == 0) return ok();
   REQUIRE(x_rows > 0, ILW_E_SHAPE, "x must have a row");
   REQUIRE(x && w && y && offsets, ILW_E_NULL, "x, w, y and offsets must not be NULL");
@@ -1613,6 +1634,226 @@ int ilw_linear_grouped(const int8_t* x, int64_t x_rows, const int32_t* rows,
   const hipError_t he = launch_grouped(a, s);
   t.done();
   return hip_status(he, "ilw_linear_grouped");
+}
+
+int ilw_quantize_rows(const int16_t* x, int64_t ld, int8_t* y, int32_t* scale, int64_t M,
+                      int32_t K, void* stream) {
+  REQUIRE(M >= 0 && K >= 16 && K % 16 == 0 && K <= 1 << 20, ILW_E_SHAPE,
+          "M=%lld must be >= 0 and K=%d a multiple of 16 in [16, 2^20]", (long long)M, K);
+  REQUIRE(ld >= K && ld % 8 == 0, ILW_E_SHAPE, "ld = %lld must be a multiple of 8 and at least %d",
+          (long long)ld, K);
+  if (M == 0) return ok();
+  REQUIRE(x && y && scale, ILW_E_NULL, "x, y and scale must not be NULL");
+  REQUIRE(aligned16(x) && aligned16(y), ILW_E_PARAM, "x and y must be 16-byte aligned");
+  QuantizeArgs a = {};
+  a.x = x;
+  a.ld = ld;
+  a.y = y;
+  a.scale = scale;
+  a.M = M;
+  a.K = K;
+  REQUIRE(quantize_rows_fits(a), ILW_E_UNSUPPORTED, "M=%lld rows of K=%d: too many for a launch",
+          (long long)M, K);
+  hipStream_t s = (hipStream_t)stream;
+  StageTimer t(ILW_STAGE_QUANTIZE, s);
+  const hipError_t he = launch_quantize_rows(a, s);
+  t.done();
+  return hip_status(he, "ilw_quantize_rows");
+}
+
+int ilw_linear_scaled(const int8_t* x, int64_t x_rows, const int32_t* x_scale,
+                      const int32_t* rows, const int32_t* offsets, const int8_t* w,
+                      const int32_t* b, ilw_dyadic rq, void* y, int32_t y_bits, int64_t M,
+                      int32_t experts, int32_t N, int32_t K, void* stream) {
+  int e;
+  if ((e = check_expert_linear(M, x_rows, rows, experts, N, K))) return e;
+  REQUIRE(y_bits == 8 || y_bits == 16, ILW_E_PARAM, "y_bits = %d must be 8 or 16", y_bits);
+  REQUIRE(offsets || experts == 1, ILW_E_SHAPE, "offsets must be given for experts = %d", experts);
+  if (M == 0) return ok();
+  REQUIRE(x_rows > 0, ILW_E_SHAPE, "x must have a row");
+  REQUIRE(x && x_scale && w && y, ILW_E_NULL, "x, x_scale, w and y must not be NULL");
+  REQUIRE(aligned16(x) && aligned16(w) && ((uintptr_t)y & 3) == 0, ILW_E_PARAM,
+          "x and w must be 16-byte aligned, y 4-byte aligned");
+  REQUIRE(rq.mult && rq.shift, ILW_E_NULL, "rq: mult/shift must not be NULL");
+  REQUIRE(rq.n == 1 || rq.n == experts * N, ILW_E_SHAPE,
+          "rq: n = %d must be 1 (one factor) or %d (one per expert and channel)", rq.n,
+          experts * N);
+  ScaledArgs a = {};
+  a.x = x;
+  a.x_scale = x_scale;
+  a.rows = rows;
+  a.offsets = offsets;
+  a.w = w;
+  a.bias = b;
+  a.mult = rq.mult;
+  a.shift = rq.shift;
+  a.y = y;
+  a.M = M;
+  a.x_rows = x_rows;
+  a.nq = rq.n;
+  a.E = experts;
+  a.N = N;
+  a.K = K;
+  a.bits = y_bits;
+  hipStream_t s = (hipStream_t)stream;
+  StageTimer t(ILW_STAGE_GEMM_SCALED, s);
+  const hipError_t he = launch_linear_scaled(a, s);
+  t.done();
+  return hip_status(he, "ilw_linear_scaled");
+}
+
+size_t ilw_route_workspace_bytes(int32_t tokens, int32_t experts) {
+  if (tokens < 0 || experts < 1 || experts > 1024) {
+    fail(ILW_E_SHAPE, "tokens = %d must be >= 0 and experts = %d in [1, 1024]", tokens, experts);
+    return 0;
+  }
+  ok();
+  return route_workspace(tokens, experts);
+}
+
+int ilw_route(const int16_t* logits, int64_t ld, const int32_t* bias, int32_t* expert,
+              int32_t* weight, int32_t* offsets, int32_t* rows, int32_t* slot, int32_t tokens,
+              int32_t experts, const ilw_route_params* rp, void* workspace,
+              size_t workspace_bytes, void* stream) {
+  REQUIRE(tokens >= 0, ILW_E_SHAPE, "tokens = %d must be >= 0", tokens);
+  REQUIRE(experts >= 1 && experts <= 1024, ILW_E_SHAPE, "experts = %d must be in [1, 1024]",
+          experts);
+  REQUIRE(ld >= experts, ILW_E_SHAPE, "ld = %lld must be at least %d", (long long)ld, experts);
+  REQUIRE(rp, ILW_E_NULL, "route parameters must not be NULL");
+  REQUIRE(rp->top_k >= 1 && rp->top_k <= 32 && rp->top_k <= experts, ILW_E_PARAM,
+          "top_k = %d must be in [1, 32] and at most %d", rp->top_k, experts);
+  REQUIRE(rp->groups >= 1 && rp->groups <= 64 && experts % rp->groups == 0, ILW_E_PARAM,
+          "groups = %d must be in [1, 64] and divide experts = %d", rp->groups, experts);
+  REQUIRE(rp->top_groups >= 1 && rp->top_groups <= rp->groups, ILW_E_PARAM,
+          "top_groups = %d must be in [1, %d]", rp->top_groups, rp->groups);
+  REQUIRE(rp->group_best == 1 || rp->group_best == 2, ILW_E_PARAM,
+          "group_best = %d must be 1 or 2", rp->group_best);
+  REQUIRE((rp->sigmoid == 0 || rp->sigmoid == 1) && (rp->renormalize == 0 || rp->renormalize == 1),
+          ILW_E_PARAM, "sigmoid = %d and renormalize = %d must be 0 or 1", rp->sigmoid,
+          rp->renormalize);
+  REQUIRE(rp->weight_mult >= 0, ILW_E_PARAM, "weight_mult = %d must be >= 0", rp->weight_mult);
+  int e;
+  if ((e = check_shift(rp->weight_shift, "weight_shift"))) return e;
+  REQUIRE((int64_t)tokens * rp->top_k < (int64_t)1 << 31, ILW_E_UNSUPPORTED,
+          "tokens * top_k = %lld must be below 2^31", (long long)tokens * rp->top_k);
+  REQUIRE(offsets, ILW_E_NULL, "offsets must not be NULL");
+  RouteArgs a = {};
+  a.logits = logits;
+  a.ld = ld;
+  a.bias = bias;
+  a.expert = expert;
+  a.weight = weight;
+  a.offsets = offsets;
+  a.rows = rows;
+  a.slot = slot;
+  a.T = tokens;
+  a.E = experts;
+  a.top_k = rp->top_k;
+  a.groups = rp->groups;
+  a.top_groups = rp->top_groups;
+  a.group_best = rp->group_best;
+  a.sigmoid = rp->sigmoid;
+  a.renorm = rp->renormalize;
+  a.mult = rp->weight_mult;
+  a.shift = rp->weight_shift;
+  const size_t need = route_workspace(tokens, experts);
+  if (tokens > 0) {
+    REQUIRE(logits && expert && weight && rows && slot, ILW_E_NULL,
+            "logits, expert, weight, rows and slot must not be NULL");
+    REQUIRE(need == 0 || (workspace && workspace_bytes >= need), ILW_E_WORKSPACE,
+            "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+  }
+  hipStream_t s = (hipStream_t)stream;
+  StageTimer t(ILW_STAGE_ROUTE, s);
+  const hipError_t he = launch_route(a, workspace, s);
+  t.done();
+  return hip_status(he, "ilw_route");
+}
+
+int ilw_combine(const void* v, int32_t bits, int64_t v_rows, const int32_t* slot,
+                const int32_t* weight, const void* skip, int32_t mult_a, int32_t mult_b,
+                int32_t shift, void* y, int64_t tokens, int32_t top_k, int32_t N, void* stream) {
+  REQUIRE(tokens >= 0 && v_rows >= 0, ILW_E_SHAPE, "tokens = %lld and v_rows = %lld must be >= 0",
+          (long long)tokens, (long long)v_rows);
+  REQUIRE(N >= 16 && N % 16 == 0 && N < 1 << 24, ILW_E_SHAPE,
+          "N = %d must be a multiple of 16, below 2^24", N);
+  REQUIRE(top_k >= 1 && top_k <= 32, ILW_E_SHAPE, "top_k = %d must be in [1, 32]", top_k);
+  REQUIRE(bits == 8 || bits == 16, ILW_E_PARAM, "bits = %d must be 8 or 16", bits);
+  int e;
+  if ((e = check_mult(mult_a, "mult_a"))) return e;
+  if ((e = check_mult(mult_b, "mult_b"))) return e;
+  if ((e = check_shift(shift, "shift"))) return e;
+  if (tokens == 0) return ok();
+  REQUIRE((v || v_rows == 0) && slot && weight && y, ILW_E_NULL,
+          "v, slot, weight and y must not be NULL");
+  REQUIRE(aligned16(v) && aligned16(skip) && aligned16(y), ILW_E_PARAM,
+          "v, skip and y must be 16-byte aligned");
+  CombineArgs a = {};
+  a.v = v;
+  a.slot = slot;
+  a.weight = weight;
+  a.skip = skip;
+  a.y = y;
+  a.v_rows = v_rows;
+  a.T = tokens;
+  a.bits = bits;
+  a.top_k = top_k;
+  a.N = N;
+  a.mult_a = mult_a;
+  a.mult_b = mult_b;
+  a.shift = shift;
+  REQUIRE(combine_fits(a), ILW_E_UNSUPPORTED, "tokens = %lld of N = %d: too many for a launch",
+          (long long)tokens, N);
+  hipStream_t s = (hipStream_t)stream;
+  StageTimer t(ILW_STAGE_COMBINE, s);
+  const hipError_t he = launch_combine(a, s);
+  t.done();
+  return hip_status(he, "ilw_combine");
+}
+
+size_t ilw_log_probs_workspace_bytes(int64_t rows, int32_t vocab, int32_t n_top) {
+  LogProbArgs a = {};
+  if (check_log_probs(rows, vocab, n_top)) return 0;
+  a.rows = rows;
+  a.V = vocab;
+  a.n_top = n_top;
+  ok();
+  return rows == 0 ? 0 : log_probs_workspace(a);
+}
+
+int ilw_log_probs(const int16_t* logits, int64_t ld, const int32_t* given, int32_t n_given,
+                  int32_t* given_lp, int32_t* entropy, int32_t* top, int32_t* top_lp,
+                  int64_t rows, int32_t vocab, int32_t n_top, void* workspace,
+                  size_t workspace_bytes, void* stream) {
+  int e;
+  if ((e = check_log_probs(rows, vocab, n_top))) return e;
+  REQUIRE(n_given >= 0 && n_given <= 64, ILW_E_SHAPE, "n_given = %d must be in [0, 64]", n_given);
+  REQUIRE(ld >= vocab, ILW_E_SHAPE, "ld = %lld must be at least %d", (long long)ld, vocab);
+  if (rows == 0) return ok();
+  REQUIRE(logits && entropy, ILW_E_NULL, "logits and entropy must not be NULL");
+  REQUIRE(n_given == 0 || (given && given_lp), ILW_E_NULL, "given and given_lp must not be NULL");
+  REQUIRE(n_top == 0 || (top && top_lp), ILW_E_NULL, "top and top_lp must not be NULL");
+  LogProbArgs a = {};
+  a.logits = logits;
+  a.ld = ld;
+  a.given = given;
+  a.given_lp = given_lp;
+  a.entropy = entropy;
+  a.top = top;
+  a.top_lp = top_lp;
+  a.rows = rows;
+  a.V = vocab;
+  a.n_given = n_given;
+  a.n_top = n_top;
+  const size_t need = log_probs_workspace(a);
+  REQUIRE(need == 0 || (workspace && workspace_bytes >= need), ILW_E_WORKSPACE,
+          "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+  REQUIRE(aligned16(workspace), ILW_E_PARAM, "workspace must be 16-byte aligned");
+  hipStream_t s = (hipStream_t)stream;
+  StageTimer t(ILW_STAGE_LOG_PROBS, s);
+  const hipError_t he = launch_log_probs(a, workspace, s);
+  t.done();
+  return hip_status(he, "ilw_log_probs");
 }
 
 int ilw_profile_enable(int enable) {

@@ -8,6 +8,7 @@ IlwError is raised.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 
@@ -18,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # ILW_LIBRARY_PATH loads another build of the same sources instead (the
 # sanitizer run of the CPU test-suite uses a host-instrumented one).
 LIB_PATH = os.environ.get("ILW_LIBRARY_PATH") or os.path.join(_HERE, "libilw.so")
-ABI_VERSION = 10
+ABI_VERSION = 11
 
 c_i32, c_i64, c_vp, c_size = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t
 
@@ -46,6 +47,11 @@ class KVCacheStruct(ctypes.Structure):
 class CacheAttnParams(ctypes.Structure):
     _fields_ = [(n, c_i32) for n in ("score_mult", "score_shift", "out_mult", "out_shift",
                                      "causal", "window")]
+
+
+class RouteParams(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("top_k", "groups", "top_groups", "group_best", "sigmoid",
+                                     "renormalize", "weight_mult", "weight_shift")]
 
 
 class BlockParams(ctypes.Structure):
@@ -133,6 +139,17 @@ _SIGS = {
                             [c_i32] * 5 + [ctypes.POINTER(CacheAttnParams), c_vp, c_size, c_vp]),
     "ilw_linear_grouped": (ctypes.c_int, [c_vp, c_i64, c_vp, c_vp, c_vp, c_vp, Dyadic, c_vp,
                                           c_i64, c_i32, c_i32, c_i32, c_vp]),
+    "ilw_quantize_rows": (ctypes.c_int, [c_vp, c_i64, c_vp, c_vp, c_i64, c_i32, c_vp]),
+    "ilw_linear_scaled": (ctypes.c_int, [c_vp, c_i64] + [c_vp] * 5 + [Dyadic, c_vp, c_i32, c_i64] +
+                          [c_i32] * 3 + [c_vp]),
+    "ilw_route_workspace_bytes": (c_size, [c_i32] * 2),
+    "ilw_route": (ctypes.c_int, [c_vp, c_i64] + [c_vp] * 6 + [c_i32] * 2 +
+                  [ctypes.POINTER(RouteParams), c_vp, c_size, c_vp]),
+    "ilw_combine": (ctypes.c_int, [c_vp, c_i32, c_i64, c_vp, c_vp, c_vp] + [c_i32] * 3 +
+                    [c_vp, c_i64, c_i32, c_i32, c_vp]),
+    "ilw_log_probs_workspace_bytes": (c_size, [c_i64, c_i32, c_i32]),
+    "ilw_log_probs": (ctypes.c_int, [c_vp, c_i64, c_vp, c_i32] + [c_vp] * 4 +
+                      [c_i64, c_i32, c_i32, c_vp, c_size, c_vp]),
     "ilw_profile_enable": (ctypes.c_int, [ctypes.c_int]),
     "ilw_profile_read": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double),
                                         ctypes.POINTER(c_i32), c_i32]),
@@ -787,9 +804,180 @@ def ilw_linear_grouped(x, w, offsets, b, mult, shift, rows=None, y=None):
     return y
 
 
+def _rows_at(t, dtype, name, device) -> int:
+    """Address of a matrix of that type on that device whose rows are contiguous."""
+    if not isinstance(t, _Tensor) or t.get_device() != device or t.dtype is not dtype or t.dim() != 2:
+        raise IlwError(f"{name} must be a matrix of {dtype} on cuda:{device}")
+    if t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1:
+        raise IlwError(f"{name} must have contiguous rows")
+    return t.data_ptr()
+
+
+def _row_step(t) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def ilw_quantize_rows(x, y=None, scale=None):
+    """x int16 [M, K] (its rows may be strided) -> y int8 [M, K], scale int32 [M]."""
+    dev = _device(x, "x")
+    at = _rows_at(x, torch.int16, "x", dev)
+    M, K = x.shape
+    if y is None:
+        y = x.new_empty((M, K), dtype=torch.int8)
+    if scale is None:
+        scale = x.new_empty((M,), dtype=torch.int32)
+    _shape(y, (M, K), "y")
+    _shape(scale, (M,), "scale")
+    rc = lib().ilw_quantize_rows(at, _row_step(x), _at(y, torch.int8, "y", dev),
+                                 _at(scale, torch.int32, "scale", dev), M, K, _raw_stream(dev))
+    _check(rc, "ilw_quantize_rows")
+    return y, scale
+
+
+def ilw_linear_scaled(x, x_scale, w, b, mult, shift, offsets=None, rows=None, bits=16, y=None):
+    """x int8 [R, K], x_scale int32 [R]; w int8 [N, K], b int32 [N] or None, mult and
+    shift int32 [1] or [N], all of them with a leading [E] and offsets int32 [E + 1] for
+    rows sorted by expert; rows int32 [M] (row of x for each row of y) or None (M = R)
+    -> int16 (bits = 16) or int8 (bits = 8) [M, N]."""
+    dev = _device(x, "x")
+    if offsets is None:
+        if w.dim() != 2:
+            raise IlwError(f"w must be [N, K], got {tuple(w.shape)}")
+        E, (N, K), lead = 1, w.shape, w.shape[:1]
+    else:
+        if w.dim() != 3:
+            raise IlwError(f"w must be [E, N, K], got {tuple(w.shape)}")
+        (E, N, K), lead = w.shape, w.shape[:2]
+        _shape(offsets, (E + 1,), "offsets")
+    if x.dim() != 2 or x.shape[1] != K:
+        raise IlwError(f"x must be [rows, {K}], got {tuple(x.shape)}")
+    R = x.shape[0]
+    _shape(x_scale, (R,), "x_scale")
+    M = R if rows is None else rows.numel()
+    if b is not None:
+        _shape(b, lead, "b")
+    n = mult.numel()
+    if shift.numel() != n:
+        raise IlwError(f"mult and shift have {n} and {shift.numel()} entries")
+    if bits != 16 and bits != 8:
+        raise IlwError(f"bits must be 8 or 16, got {bits}")
+    dtype = torch.int16 if bits == 16 else torch.int8
+    if y is None:
+        y = x.new_empty((M, N), dtype=dtype)
+    _shape(y, (M, N), "y")
+    rc = lib().ilw_linear_scaled(
+        _at(x, torch.int8, "x", dev), R, _at(x_scale, torch.int32, "x_scale", dev),
+        None if rows is None else _at(rows, torch.int32, "rows", dev),
+        None if offsets is None else _at(offsets, torch.int32, "offsets", dev),
+        _at(w, torch.int8, "w", dev), None if b is None else _at(b, torch.int32, "b", dev),
+        Dyadic(_at(mult, torch.int32, "mult", dev), _at(shift, torch.int32, "shift", dev), n),
+        _at(y, dtype, "y", dev), bits, M, E, N, K, _raw_stream(dev))
+    _check(rc, "ilw_linear_scaled")
+    return y
+
+
+# expert, weight, slot int32 [T, top_k], offsets int32 [E + 1], rows int32 [T * top_k]
+Routing = collections.namedtuple("Routing", "expert weight offsets rows slot")
+
+
+def ilw_route(logits, top_k, bias=None, sigmoid=False, renormalize=True, groups=1, top_groups=1,
+              group_best=2, weight_mult=1 << 30, weight_shift=44, workspace=None):
+    """logits int16 [T, E] in 1/64 octave (rows may be strided; -32768: not to be had),
+    bias int32 [E] in 2^-30 or None -> Routing.  Weights are in 2^-16 with the default
+    factor.  offsets and rows go to ilw_linear_grouped and ilw_linear_scaled, slot and
+    weight to ilw_combine."""
+    dev = _device(logits, "logits")
+    at = _rows_at(logits, torch.int16, "logits", dev)
+    T, E = logits.shape
+    if bias is not None:
+        _shape(bias, (E,), "bias")
+    L = lib()
+    if workspace is None:
+        need = L.ilw_route_workspace_bytes(T, E)
+        workspace = torch.empty(need, dtype=torch.int8, device=logits.device) if need else None
+    # one allocation for the five results: offsets last, so that the others stay aligned
+    n = T * top_k if top_k > 0 else 0
+    out = logits.new_empty((4 * n + E + 1,), dtype=torch.int32)
+    p = out.data_ptr()
+    rp = RouteParams(top_k, groups, top_groups, group_best, sigmoid, renormalize, weight_mult,
+                     weight_shift)
+    rc = L.ilw_route(at, _row_step(logits),
+                     None if bias is None else _at(bias, torch.int32, "bias", dev), p, p + 4 * n,
+                     p + 16 * n, p + 8 * n, p + 12 * n, T, E, rp,
+                     None if workspace is None else _at(workspace, torch.int8, "workspace", dev),
+                     0 if workspace is None else workspace.numel(), _raw_stream(dev))
+    _check(rc, "ilw_route")
+    expert, weight, rows, slot, offsets = out.split([n, n, n, n, E + 1])
+    return Routing(expert.view(T, top_k), weight.view(T, top_k), offsets, rows,
+                   slot.view(T, top_k))
+
+
+def ilw_combine(v, slot, weight, mult, shift, skip=None, skip_mult=0, y=None):
+    """v int8 or int16 [R, N], slot and weight int32 [T, top_k], skip [T, N] as v or None
+    -> y [T, N] as v (y may be skip): sat(rq2(sum of weight v in 2^-8, mult, skip,
+    skip_mult; shift))."""
+    dev = _device(v, "v")
+    if v.dim() != 2 or slot.dim() != 2:
+        raise IlwError(f"v and slot must be matrices, got {tuple(v.shape)} and {tuple(slot.shape)}")
+    (R, N), (T, top_k) = v.shape, slot.shape
+    if v.dtype is not torch.int8 and v.dtype is not torch.int16:
+        raise IlwError(f"v must be int8 or int16, got {v.dtype}")
+    _shape(weight, (T, top_k), "weight")
+    if skip is not None:
+        _shape(skip, (T, N), "skip")
+    if y is None:
+        y = v.new_empty((T, N))
+    _shape(y, (T, N), "y")
+    dt = v.dtype
+    rc = lib().ilw_combine(
+        _at(v, dt, "v", dev), 8 if dt is torch.int8 else 16, R,
+        _at(slot, torch.int32, "slot", dev), _at(weight, torch.int32, "weight", dev),
+        None if skip is None else _at(skip, dt, "skip", dev), mult, skip_mult, shift,
+        _at(y, dt, "y", dev), T, top_k, N, _raw_stream(dev))
+    _check(rc, "ilw_combine")
+    return y
+
+
+# given, int32 [rows, n_given]; entropy int32 [rows]; top, top_log_prob int32 [rows, n_top]
+LogProbs = collections.namedtuple("LogProbs", "given entropy top top_log_prob")
+
+
+def ilw_log_probs(logits, given=None, top=0, workspace=None):
+    """logits int16 [rows, vocab] in 1/64 octave (rows may be strided; -32768: not to be
+    had), given int32 [rows, n] token numbers or None -> LogProbs: log2 probabilities of
+    the given tokens, the entropy in bits, the `top` best tokens and their log2
+    probabilities, all but the token numbers in 2^-16."""
+    dev = _device(logits, "logits")
+    at = _rows_at(logits, torch.int16, "logits", dev)
+    rows, vocab = logits.shape
+    n = 0
+    if given is not None:
+        if given.dim() != 2 or given.shape[0] != rows:
+            raise IlwError(f"given must be [{rows}, tokens], got {tuple(given.shape)}")
+        n = given.shape[1]
+    L = lib()
+    if workspace is None:
+        need = L.ilw_log_probs_workspace_bytes(rows, vocab, top)
+        if need == 0 and last_error():
+            raise IlwError(f"ilw_log_probs_workspace_bytes: {last_error()}")
+        workspace = torch.empty(need, dtype=torch.int8, device=logits.device) if need else None
+    new = logits.new_empty
+    out = LogProbs(new((rows, n), dtype=torch.int32), new((rows,), dtype=torch.int32),
+                   new((rows, top), dtype=torch.int32), new((rows, top), dtype=torch.int32))
+    rc = L.ilw_log_probs(
+        at, _row_step(logits), None if n == 0 else _at(given, torch.int32, "given", dev), n,
+        out.given.data_ptr(), out.entropy.data_ptr(), out.top.data_ptr(),
+        out.top_log_prob.data_ptr(), rows, vocab, top,
+        None if workspace is None else _at(workspace, torch.int8, "workspace", dev),
+        0 if workspace is None else workspace.numel(), _raw_stream(dev))
+    _check(rc, "ilw_log_probs")
+    return out
+
+
 STAGES = ["layernorm", "gemm_qkv", "attention", "gemm_proj", "gemm_fc1", "gemm_fc2",
           "relayout", "deform", "block_tail", "split_conv", "patch_embed", "decoder", "tail384",
-          "cache_append", "cache_attention", "gemm_grouped"]
+          "cache_append", "cache_attention", "gemm_grouped", "quantize", "gemm_scaled", "route",
+          "combine", "log_probs"]
 
 
 def profile_enable(on: bool = True):
