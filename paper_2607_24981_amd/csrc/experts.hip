@@ -4,23 +4,57 @@
 // sigmoid, 2^(-a/64) from a table of 64 values), the choice goes by probability +
 // bias within the groups that are kept, and the (token, choice) pairs are sorted by
 // expert, then by token.
-//   choose_kernel  a wave a token: probabilities, groups, the best top_k; a
-//                  workgroup of 64 tokens counts its choices of each expert
+//   choose_kernel  a wave a token, NV neighbouring experts a lane; the best is found
+//                  top_k times: the lanes' maxima by DPP, then the lowest lane that
+//                  has it, which is the lowest index
 //   place_kernel   each workgroup sums the counts of the workgroups before it and
-//                  all of them, which gives every expert's start, and places its 64
-//                  tokens: the rank of a token among those of the workgroup that
-//                  chose an expert is a popcount of the expert's 64-bit set
-// 64 tokens or fewer are chosen and placed by one workgroup in one launch.  No
+//                  all of them, which gives every expert's start, and places its
+//                  tokens 64 at a time: the rank of a token among the 64 that chose
+//                  an expert is a popcount of the expert's 64-bit set
+// 64 tokens or fewer are chosen and placed by one workgroup in one launch.  At most
+// MAXB workgroups share the tokens, so that the counts they all read stay few.  No
 // counter is shared between workgroups: the order does not depend on their timing.
 #include "step_internal.h"
 
 namespace ilw {
 namespace {
 
-constexpr int NT = 256, WAVES = NT / 64;
-constexpr int TB = 64;  // tokens a workgroup
+constexpr int NT = 1024, WAVES = NT / 64;
+constexpr int TB = 64;     // tokens of a set
+constexpr int MAXB = 256;  // workgroups
+constexpr int MAXE = 1024;
 
-// Probabilities of the NV scores a lane has (experts lane + 64 i) in 2^-30.
+// Wave-wide results in every lane (scalar), by DPP within rows of 16 lanes and from
+// row to row: 6 vector instructions where exchanges through LDS take 6 round trips.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int32_t dpp_or(int32_t old, int32_t v) {
+  return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int32_t scalar_max(int32_t v) {
+  v = max(v, dpp_or<0x111, 0xf>(v, v));  // row_shr 1, 2, 4, 8
+  v = max(v, dpp_or<0x112, 0xf>(v, v));
+  v = max(v, dpp_or<0x114, 0xf>(v, v));
+  v = max(v, dpp_or<0x118, 0xf>(v, v));
+  v = max(v, dpp_or<0x142, 0xa>(v, v));  // row_bcast 15, 31
+  v = max(v, dpp_or<0x143, 0xc>(v, v));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ uint32_t scalar_sum(uint32_t u) {
+  int32_t v = (int32_t)u;
+  v += dpp_or<0x111, 0xf>(0, v);
+  v += dpp_or<0x112, 0xf>(0, v);
+  v += dpp_or<0x114, 0xf>(0, v);
+  v += dpp_or<0x118, 0xf>(0, v);
+  v += dpp_or<0x142, 0xa>(0, v);
+  v += dpp_or<0x143, 0xc>(0, v);
+  return (uint32_t)__builtin_amdgcn_readlane(v, 63);
+}
+// Of values below 2^36.
+__device__ __forceinline__ uint64_t scalar_sum_u64(uint64_t v) {
+  return ((uint64_t)scalar_sum((uint32_t)(v >> 20)) << 20) + scalar_sum((uint32_t)v & 0xfffffu);
+}
+
+// Probabilities of a lane's NV scores in 2^-30.
 template <int NV>
 __device__ __forceinline__ void probabilities(const int32_t (&s)[NV], uint32_t (&p)[NV],
                                               bool sigmoid, const uint32_t* table) {
@@ -36,14 +70,14 @@ __device__ __forceinline__ void probabilities(const int32_t (&s)[NV], uint32_t (
   int32_t top = kNoScore;
 #pragma unroll
   for (int i = 0; i < NV; ++i) top = max(top, s[i]);
-  top = wave_max_i32(top);
+  top = scalar_max(top);
   uint64_t sum = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     p[i] = s[i] == kNoScore ? 0 : exp2_q30(table, (uint32_t)(top - s[i]));
     sum += p[i];
   }
-  sum = wave_sum_u64(sum);
+  sum = scalar_sum_u64(sum);
   if (sum == 0) return;  // no expert to be had
   const int32_t d = bit_length(sum) - 31;
   const uint32_t f = inverse_2p62((uint32_t)(sum >> d));
@@ -51,86 +85,98 @@ __device__ __forceinline__ void probabilities(const int32_t (&s)[NV], uint32_t (
   for (int i = 0; i < NV; ++i) p[i] = __umulhi(p[i], f) >> d;
 }
 
-// Leaves in c (INT32_MIN: none) only the experts of the top_groups best groups.
-// `best` is the wave's LDS for E values.
+// How the groups lie on the lanes: `sub` lanes, a power of two, go over a group's
+// experts; bit at of the kept set is that of the group of a lane's expert i.
 template <int NV>
-__device__ __forceinline__ void keep_groups(const RouteArgs& a, int32_t (&c)[NV], int32_t* best,
-                                            int lane) {
-  const int32_t per = a.E / a.groups;
+struct Groups {
+  int32_t per, sub, log_sub;
+  int32_t at[NV];
+  __device__ __forceinline__ void init(const RouteArgs& a, int lane) {
+    per = a.E / a.groups;
+    log_sub = 6 - (32 - __clz(a.groups - 1));  // groups > 1
+    sub = 1 << log_sub;
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
-    if (lane + 64 * i < a.E) best[lane + 64 * i] = c[i];
+    for (int i = 0; i < NV; ++i)
+      at[i] = (min((lane * NV + i) / per, a.groups - 1)) << log_sub;
+  }
+};
+
+// Leaves in c (INT32_MIN: none) only the experts of the top_groups best groups.
+// `lds` is the wave's, for E values.
+template <int NV>
+__device__ __forceinline__ void keep_groups(const RouteArgs& a, const Groups<NV>& g,
+                                            int32_t (&c)[NV], int32_t* lds, int lane) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i) lds[lane * NV + i] = c[i];
   __builtin_amdgcn_wave_barrier();
-  // a group is a lane's: its best one or two
-  int32_t b0 = INT32_MIN, b1 = INT32_MIN;
-  if (lane < a.groups)
-    for (int32_t i = 0; i < per; ++i) {
-      const int32_t v = best[lane * per + i];
+  const int32_t group = lane >> g.log_sub;
+  int32_t b0 = INT32_MIN, b1 = INT32_MIN;  // the best two
+  if (group < a.groups)
+    for (int32_t i = lane & (g.sub - 1); i < g.per; i += g.sub) {
+      const int32_t v = lds[group * g.per + i];
       b1 = max(b1, min(b0, v));
       b0 = max(b0, v);
     }
   __builtin_amdgcn_wave_barrier();
+  for (int32_t o = 1; o < g.sub; o <<= 1) {
+    const int32_t o0 = __shfl_xor(b0, o, 64), o1 = __shfl_xor(b1, o, 64);
+    b1 = max(max(b1, o1), min(b0, o0));
+    b0 = max(b0, o0);
+  }
   const int64_t score =
       b0 == INT32_MIN ? INT64_MIN : (int64_t)b0 + (a.group_best == 2 && b1 != INT32_MIN ? b1 : 0);
   int32_t rank = 0;
-  for (int32_t g = 0; g < a.groups; ++g) {
-    const int64_t other = (int64_t)(((uint64_t)(uint32_t)__shfl((int32_t)(score >> 32), g, 64) << 32) |
-                                    (uint32_t)__shfl((int32_t)score, g, 64));
-    rank += other > score || (other == score && g < lane);
+  for (int32_t h = 0; h < a.groups; ++h) {
+    const int32_t l = h << g.log_sub;
+    const int64_t other =
+        (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int32_t)(score >> 32), l) << 32) |
+                  (uint32_t)__builtin_amdgcn_readlane((int32_t)score, l));
+    rank += other > score || (other == score && h < group);
   }
-  const uint64_t kept = __ballot(lane < a.groups && b0 != INT32_MIN && rank < a.top_groups);
+  const uint64_t kept = __ballot(group < a.groups && b0 != INT32_MIN && rank < a.top_groups);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int32_t e = lane + 64 * i;
-    if (e < a.E && !(kept >> (e / per) & 1)) c[i] = INT32_MIN;
-  }
+  for (int i = 0; i < NV; ++i) c[i] = (kept >> g.at[i]) & 1 ? c[i] : INT32_MIN;
 }
 
 // The choices of token t: writes expert and weight, enters them in the sets.
 template <int NV>
-__device__ __forceinline__ void choose(const RouteArgs& a, int32_t t, int32_t bit, int lane,
-                                       const uint32_t* table, int32_t* best,
+__device__ __forceinline__ void choose(const RouteArgs& a, const Groups<NV>& g,
+                                       const int32_t (&bias)[NV], int32_t t, int32_t bit, int lane,
+                                       const uint32_t* table, int32_t* lds,
                                        unsigned long long* sets) {
   int32_t s[NV], c[NV];
   uint32_t p[NV];
   const int16_t* row = a.logits + (int64_t)t * a.ld;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) s[i] = lane + 64 * i < a.E ? row[lane + 64 * i] : kNoScore;
+  for (int i = 0; i < NV; ++i) s[i] = lane * NV + i < a.E ? row[lane * NV + i] : kNoScore;
   probabilities<NV>(s, p, a.sigmoid, table);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int32_t e = lane + 64 * i;
-    const int32_t b = a.bias && e < a.E ? min(max(a.bias[e], -(1 << 30)), 1 << 30) : 0;
-    c[i] = s[i] == kNoScore ? INT32_MIN : (int32_t)p[i] + b;
-  }
-  if (a.groups > 1) keep_groups<NV>(a, c, best, lane);
+  for (int i = 0; i < NV; ++i) c[i] = s[i] == kNoScore ? INT32_MIN : (int32_t)p[i] + bias[i];
+  if (a.groups > 1) keep_groups<NV>(a, g, c, lds, lane);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) lds[lane * NV + i] = (int32_t)p[i];
+  __builtin_amdgcn_wave_barrier();
   int32_t expert = -1;  // lane j: choice j
-  uint32_t prob = 0;
   for (int32_t j = 0; j < a.top_k; ++j) {
     int32_t m = c[0];
 #pragma unroll
     for (int i = 1; i < NV; ++i) m = max(m, c[i]);
-    m = wave_max_i32(m);
-    if (m == INT32_MIN) break;
-    bool found = false;
+    const int32_t best = scalar_max(m);
+    if (best == INT32_MIN) break;
+    const int l = __ffsll((unsigned long long)__ballot(m == best)) - 1;
+    int32_t which = 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const uint64_t hit = __ballot(c[i] == m);
-      if (!found && hit) {
-        found = true;
-        const int l = __ffsll((unsigned long long)hit) - 1;
-        const uint32_t pj = __builtin_amdgcn_readlane(p[i], l);
-        if (lane == l) c[i] = INT32_MIN;
-        if (lane == j) {
-          expert = l + 64 * i;
-          prob = pj;
-        }
-      }
-    }
+    for (int i = NV - 1; i >= 0; --i) which = c[i] == best ? i : which;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) c[i] = lane == l && which == i ? INT32_MIN : c[i];
+    const int32_t e = l * NV + __builtin_amdgcn_readlane(which, l);
+    expert = lane == j ? e : expert;
   }
+  const uint32_t prob = expert >= 0 ? (uint32_t)lds[expert] : 0;
+  __builtin_amdgcn_wave_barrier();
   uint32_t r = prob;
   if (a.renorm) {
-    const uint64_t sum = wave_sum_u64(prob);
+    const uint64_t sum = scalar_sum_u64(prob);
     const int32_t n = bit_length(sum);
     if (sum) {
       const uint32_t unit = (uint32_t)(n <= 31 ? sum << (31 - n) : sum >> (n - 31));
@@ -138,7 +184,8 @@ __device__ __forceinline__ void choose(const RouteArgs& a, int32_t t, int32_t bi
     }
   }
   if (lane < a.top_k) {
-    const int64_t w = ((int64_t)((uint64_t)r * (uint32_t)a.mult) + ((int64_t)1 << (a.shift - 1))) >> a.shift;
+    const int64_t w =
+        ((int64_t)((uint64_t)r * (uint32_t)a.mult) + ((int64_t)1 << (a.shift - 1))) >> a.shift;
     const int64_t at = (int64_t)t * a.top_k + lane;
     a.expert[at] = expert;
     a.weight[at] = (int32_t)min(w, (int64_t)INT32_MAX);
@@ -163,13 +210,13 @@ __device__ __forceinline__ int32_t starts(int32_t* total, int32_t E, int lane) {
   return before;
 }
 
-// Places the workgroup's tokens: start[e] is the row of its first token of expert e.
+// Places TB tokens from t0 on: start[e] is the row of the first that chose e.
 __device__ __forceinline__ void place(const RouteArgs& a, int32_t t0, const int32_t* start,
-                                      const unsigned long long* sets, const int32_t* expert) {
+                                      const unsigned long long* sets) {
   const int32_t n = min(TB, a.T - t0) * a.top_k;
-  for (int32_t i = threadIdx.x; i < n; i += blockDim.x) {
+  for (int32_t i = threadIdx.x; i < n; i += NT) {
     const int64_t at = (int64_t)t0 * a.top_k + i;
-    const int32_t e = expert[at], t = i / a.top_k;
+    const int32_t e = a.expert[at], t = i / a.top_k;
     int32_t slot = -1;
     if (e >= 0) {
       slot = start[e] + __popcll(sets[e] & (((unsigned long long)1 << t) - 1));
@@ -179,84 +226,109 @@ __device__ __forceinline__ void place(const RouteArgs& a, int32_t t0, const int3
   }
 }
 
+// Workgroup b has the sets b * per .. b * per + per - 1.
 template <int NV, bool ONE>
-__global__ __launch_bounds__(NT) void choose_kernel(RouteArgs a, uint8_t* counts) {
+__global__ __launch_bounds__(NT) void choose_kernel(RouteArgs a, int32_t* counts, int32_t per) {
   __shared__ uint32_t table[64];
   __shared__ unsigned long long sets[64 * NV];
-  __shared__ int32_t best[WAVES][64 * NV];
+  __shared__ int32_t lds[WAVES][64 * NV];
   __shared__ int32_t used;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int32_t t0 = blockIdx.x * TB, n = min(TB, a.T - t0);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   load_exp2(table);
-  for (int32_t e = tid; e < a.E; e += NT) sets[e] = 0;
+  for (int32_t e = tid; e < 64 * NV; e += NT) sets[e] = 0;
+  int32_t bias[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    bias[i] = a.bias && lane * NV + i < a.E
+                  ? min(max(a.bias[lane * NV + i], -(1 << 30)), 1 << 30) : 0;
+  Groups<NV> g;
+  if (a.groups > 1) g.init(a, lane);
   __syncthreads();
-  for (int32_t t = wave; t < n; t += WAVES)
-    choose<NV>(a, t0 + t, t, lane, table, best[wave], sets);
-  __syncthreads();
+  int32_t count = 0;  // of expert tid
+  for (int32_t k = 0; k < per; ++k) {
+    const int64_t first = ((int64_t)blockIdx.x * per + k) * TB;
+    if (first >= a.T && !ONE) break;
+    const int32_t t0 = (int32_t)first;
+    const int32_t n = min(TB, a.T - t0);
+    for (int32_t t = wave; t < n; t += WAVES)
+      choose<NV>(a, g, bias, t0 + t, t, lane, table, lds[wave], sets);
+    if (ONE) break;
+    __syncthreads();
+    if (tid < 64 * NV) {
+      count += __popcll(sets[tid]);
+      sets[tid] = 0;
+    }
+    __syncthreads();
+  }
   if (!ONE) {
-    for (int32_t e = tid; e < a.E; e += NT)
-      counts[(int64_t)blockIdx.x * a.E + e] = (uint8_t)__popcll(sets[e]);
+    if (tid < a.E) counts[(int64_t)blockIdx.x * a.E + tid] = count;
     return;
   }
-  int32_t* start = best[0];
-  for (int32_t e = tid; e < a.E; e += NT) start[e] = __popcll(sets[e]);
+  __syncthreads();
+  int32_t* start = lds[0];
+  if (tid < a.E) start[tid] = __popcll(sets[tid]);
   __syncthreads();
   if (wave == 0) {
     const int32_t all = starts(start, a.E, lane);
     if (lane == 0) used = a.offsets[a.E] = all;
   }
   __syncthreads();
-  for (int32_t e = tid; e < a.E; e += NT) a.offsets[e] = start[e];
-  place(a, t0, start, sets, a.expert);  // (this workgroup's own stores, before barriers)
+  if (tid < a.E) a.offsets[tid] = start[tid];
+  place(a, 0, start, sets);  // (the workgroup's own stores, before barriers)
   for (int32_t i = used + tid; i < a.T * a.top_k; i += NT) a.rows[i] = -1;
 }
 
-constexpr int MAXE = 1024;
-
-__global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const uint8_t* counts) {
+__global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const int32_t* counts, int32_t per) {
   __shared__ unsigned long long sets[MAXE];
-  __shared__ int32_t start[MAXE];
+  __shared__ int32_t start[MAXE], before[MAXE];
   __shared__ int32_t used;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int32_t b = blockIdx.x, nb = gridDim.x, t0 = b * TB;
-  int32_t before[MAXE / NT];
-#pragma unroll
-  for (int i = 0; i < MAXE / NT; ++i) {
-    const int32_t e = tid + i * NT;
-    before[i] = 0;
-    if (e < a.E) {
-      int32_t all = 0;
-      for (int32_t k = 0; k < nb; ++k) {
-        const int32_t c = counts[(int64_t)k * a.E + e];
-        before[i] += k < b ? c : 0;
-        all += c;
-      }
-      sets[e] = 0;
-      start[e] = all;
+  const int32_t b = blockIdx.x, nb = gridDim.x;
+  start[tid] = before[tid] = 0;
+  sets[tid] = 0;
+  __syncthreads();
+  // cols threads side by side take an expert each, NT / cols rows of counts at a time
+  const int32_t cols = a.E > 512 ? 1024 : a.E > 256 ? 512 : a.E > 128 ? 256 : a.E > 64 ? 128 : 64;
+  const int32_t e = tid & (cols - 1), step = NT / cols;
+  if (e < a.E) {
+    int32_t all = 0, mine = 0;
+#pragma unroll 8
+    for (int32_t k = tid / cols; k < nb; k += step) {
+      const int32_t c = counts[k * a.E + e];
+      all += c;
+      mine += k < b ? c : 0;
     }
+    atomicAdd(&start[e], all);  // (whole numbers: in any order)
+    atomicAdd(&before[e], mine);
   }
   __syncthreads();
   if (wave == 0) {
     const int32_t all = starts(start, a.E, lane);
     if (lane == 0) used = all;
   }
-  const int32_t n = min(TB, a.T - t0) * a.top_k;
-  for (int32_t i = tid; i < n; i += NT) {
-    const int32_t e = a.expert[(int64_t)t0 * a.top_k + i];
-    if (e >= 0) atomicOr(&sets[e], 1ull << (i / a.top_k));
-  }
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < MAXE / NT; ++i) {
-    const int32_t e = tid + i * NT;
-    if (e < a.E) {
-      if (b == 0) a.offsets[e] = start[e];
-      start[e] += before[i];
+  if (b == 0) {
+    if (tid < a.E) a.offsets[tid] = start[tid];
+    if (tid == 0) a.offsets[a.E] = used;
+  }
+  start[tid] += before[tid];
+  for (int32_t k = 0; k < per; ++k) {
+    const int64_t first = ((int64_t)b * per + k) * TB;
+    if (first >= a.T) break;
+    const int32_t t0 = (int32_t)first;
+    const int32_t n = min(TB, a.T - t0) * a.top_k;
+    __syncthreads();
+    for (int32_t i = tid; i < n; i += NT) {
+      const int32_t x = a.expert[(int64_t)t0 * a.top_k + i];
+      if (x >= 0) atomicOr(&sets[x], 1ull << (i / a.top_k));
     }
+    __syncthreads();
+    place(a, t0, start, sets);
+    __syncthreads();
+    start[tid] += __popcll(sets[tid]);
+    sets[tid] = 0;
   }
-  if (b == 0 && tid == 0) a.offsets[a.E] = used;
-  __syncthreads();
-  place(a, t0, start, sets, a.expert);
   const int64_t all = (int64_t)a.T * a.top_k;
   for (int64_t i = used + (int64_t)b * NT + tid; i < all; i += (int64_t)nb * NT) a.rows[i] = -1;
 }
@@ -264,12 +336,14 @@ __global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const uint8_t* c
 // ------------------------------------------------------------------- combine
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int CT = 256, CWAVES = CT / 64;
+
 // A wave has 64 units of 16 bytes of a token's row.
 template <int BYTES>
-__global__ __launch_bounds__(NT) void combine_kernel(CombineArgs a, int32_t parts) {
+__global__ __launch_bounds__(CT) void combine_kernel(CombineArgs a, int32_t parts) {
   constexpr int VALS = 16 / BYTES, lim = BYTES == 1 ? 127 : 32767;
   const int lane = threadIdx.x & 63;
-  const int64_t wave = (int64_t)blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t wave = (int64_t)blockIdx.x * CWAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t t = wave / parts;
   const int32_t unit = (int32_t)(wave - t * parts) * 64 + lane;
   const int64_t ld = (int64_t)a.N * BYTES;
@@ -312,20 +386,30 @@ int32_t combine_parts(const CombineArgs& a) { return (a.N * (a.bits / 8) / 16 + 
 
 }  // namespace
 
+// Sets of 64 tokens that a workgroup has.
+static int32_t route_sets(int32_t T) {
+  const int32_t sets = T > 0 ? (T - 1) / TB + 1 : 1;  // (no token: offsets of 0)
+  return (sets - 1) / MAXB + 1;
+}
+static int32_t route_blocks(int32_t T) {
+  const int32_t tokens = TB * route_sets(T);
+  return T > 0 ? (T - 1) / tokens + 1 : 1;
+}
+
 size_t route_workspace(int32_t T, int32_t E) {
-  const int64_t blocks = ((int64_t)T + TB - 1) / TB;
-  return blocks <= 1 ? 0 : (size_t)(blocks * E);
+  const int32_t blocks = route_blocks(T);
+  return blocks == 1 ? 0 : (size_t)blocks * E * sizeof(int32_t);
 }
 
 hipError_t launch_route(const RouteArgs& a, void* ws, hipStream_t s) {
-  const int32_t blocks = a.T > 0 ? (a.T - 1) / TB + 1 : 1;  // (no token: offsets of 0)
-  uint8_t* counts = (uint8_t*)ws;
+  const int32_t per = route_sets(a.T), blocks = route_blocks(a.T);
+  int32_t* counts = (int32_t*)ws;
   const auto choose_with = [&](auto nv) {
     constexpr int NV = decltype(nv)::value;
     if (blocks == 1)
-      hipLaunchKernelGGL((choose_kernel<NV, true>), dim3(1), dim3(NT), 0, s, a, counts);
+      hipLaunchKernelGGL((choose_kernel<NV, true>), dim3(1), dim3(NT), 0, s, a, counts, per);
     else
-      hipLaunchKernelGGL((choose_kernel<NV, false>), dim3(blocks), dim3(NT), 0, s, a, counts);
+      hipLaunchKernelGGL((choose_kernel<NV, false>), dim3(blocks), dim3(NT), 0, s, a, counts, per);
   };
   if (a.E <= 64) choose_with(IntC<1>{});
   else if (a.E <= 128) choose_with(IntC<2>{});
@@ -334,21 +418,21 @@ hipError_t launch_route(const RouteArgs& a, void* ws, hipStream_t s) {
   else choose_with(IntC<16>{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || blocks == 1) return e;
-  hipLaunchKernelGGL(place_kernel, dim3(blocks), dim3(NT), 0, s, a, counts);
+  hipLaunchKernelGGL(place_kernel, dim3(blocks), dim3(NT), 0, s, a, counts, per);
   return hipGetLastError();
 }
 
 bool combine_fits(const CombineArgs& a) {
-  return (a.T * combine_parts(a) + WAVES - 1) / WAVES < (int64_t)1 << 24;
+  return (a.T * combine_parts(a) + CWAVES - 1) / CWAVES < (int64_t)1 << 24;
 }
 
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s) {
   const int32_t parts = combine_parts(a);
-  const int64_t blocks = (a.T * parts + WAVES - 1) / WAVES;
+  const int64_t blocks = (a.T * parts + CWAVES - 1) / CWAVES;
   if (a.bits == 8)
-    hipLaunchKernelGGL((combine_kernel<1>), dim3((unsigned)blocks), dim3(NT), 0, s, a, parts);
+    hipLaunchKernelGGL((combine_kernel<1>), dim3((unsigned)blocks), dim3(CT), 0, s, a, parts);
   else
-    hipLaunchKernelGGL((combine_kernel<2>), dim3((unsigned)blocks), dim3(NT), 0, s, a, parts);
+    hipLaunchKernelGGL((combine_kernel<2>), dim3((unsigned)blocks), dim3(CT), 0, s, a, parts);
   return hipGetLastError();
 }
 
