@@ -631,8 +631,9 @@ int ilw_linear_scaled(const int8_t* x, int64_t x_rows, const int32_t* x_scale,
  *            take.
  * experts in [1, 1024], a multiple of groups; groups in [1, 64], top_groups in [1,
  * groups]; top_k in [1, min(32, experts)]; weight_mult in [0, 2^31), weight_shift in
- * [1, 62]; tokens * top_k < 2^31.  At most two launches.  The workspace may hold
- * anything; calls that may run at the same time need one each.
+ * [1, 62]; tokens * top_k < 2^31.  At most two launches.  The workspace (16-byte
+ * aligned, its size may be 0) may hold anything; calls that may run at the same time
+ * need one each.
  */
 typedef struct {
   int32_t top_k, groups, top_groups, group_best;

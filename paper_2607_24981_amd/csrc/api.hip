@@ -1762,6 +1762,7 @@ int ilw_route(const int16_t* logits, int64_t ld, const int32_t* bias, int32_t* e
             "logits, expert, weight, rows and slot must not be NULL");
     REQUIRE(need == 0 || (workspace && workspace_bytes >= need), ILW_E_WORKSPACE,
             "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+    REQUIRE(aligned16(workspace), ILW_E_PARAM, "workspace must be 16-byte aligned");
   }
   hipStream_t s = (hipStream_t)stream;
   StageTimer t(ILW_STAGE_ROUTE, s);

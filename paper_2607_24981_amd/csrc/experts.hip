@@ -4,9 +4,9 @@
 // sigmoid, 2^(-a/64) from a table of 64 values), the choice goes by probability +
 // bias within the groups that are kept, and the (token, choice) pairs are sorted by
 // expert, then by token.
-//   choose_kernel  a wave a token, NV neighbouring experts a lane; the best is found
-//                  top_k times: the lanes' maxima by DPP, then the lowest lane that
-//                  has it, which is the lowest index
+//   choose_kernel  a wave a token, NV neighbouring experts a lane, sorted there; the
+//                  best is found top_k times: the largest of the lanes' first by DPP,
+//                  then the lowest lane that has it, which is the lowest index
 //   place_kernel   each workgroup sums the counts of the workgroups before it and
 //                  all of them, which gives every expert's start, and places its
 //                  tokens 64 at a time: the rank of a token among the 64 that chose
@@ -31,12 +31,12 @@ __device__ __forceinline__ int32_t dpp_or(int32_t old, int32_t v) {
   return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xf, false);
 }
 __device__ __forceinline__ int32_t scalar_max(int32_t v) {
-  v = max(v, dpp_or<0x111, 0xf>(v, v));  // row_shr 1, 2, 4, 8
-  v = max(v, dpp_or<0x112, 0xf>(v, v));
-  v = max(v, dpp_or<0x114, 0xf>(v, v));
-  v = max(v, dpp_or<0x118, 0xf>(v, v));
-  v = max(v, dpp_or<0x142, 0xa>(v, v));  // row_bcast 15, 31
-  v = max(v, dpp_or<0x143, 0xc>(v, v));
+  v = max(v, dpp_or<0x111, 0xf>(INT32_MIN, v));  // row_shr 1, 2, 4, 8
+  v = max(v, dpp_or<0x112, 0xf>(INT32_MIN, v));
+  v = max(v, dpp_or<0x114, 0xf>(INT32_MIN, v));
+  v = max(v, dpp_or<0x118, 0xf>(INT32_MIN, v));
+  v = max(v, dpp_or<0x142, 0xa>(INT32_MIN, v));  // row_bcast 15, 31
+  v = max(v, dpp_or<0x143, 0xc>(INT32_MIN, v));
   return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ uint32_t scalar_sum(uint32_t u) {
@@ -85,44 +85,91 @@ __device__ __forceinline__ void probabilities(const int32_t (&s)[NV], uint32_t (
   for (int i = 0; i < NV; ++i) p[i] = __umulhi(p[i], f) >> d;
 }
 
-// How the groups lie on the lanes: `sub` lanes, a power of two, go over a group's
-// experts; bit at of the kept set is that of the group of a lane's expert i.
+// A score and its lane's index of it, ordered by score, then by lower index.
+struct Scored {
+  int32_t c, i;
+};
+__device__ __forceinline__ int64_t order_of(const Scored& x) {
+  return (int64_t)(((uint64_t)(uint32_t)x.c << 32) | (uint32_t)~x.i);
+}
+// Best first, by odd-even merging.
+template <int NV>
+__device__ __forceinline__ void sort_lane(Scored (&x)[NV]) {
+#pragma unroll
+  for (int p = 1; p < NV; p <<= 1)
+#pragma unroll
+    for (int k = p; k >= 1; k >>= 1)
+#pragma unroll
+      for (int j = k % p; j + k < NV; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; ++i) {
+          const int l = j + i, r = j + i + k;
+          if (r < NV && l / (2 * p) == r / (2 * p)) {
+            const bool swap = order_of(x[l]) < order_of(x[r]);
+            const Scored u = swap ? x[r] : x[l], v = swap ? x[l] : x[r];
+            x[l] = u;
+            x[r] = v;
+          }
+        }
+}
+
+template <int NV>
+struct Order {
+  typedef uint32_t type;
+};
+template <>
+struct Order<16> {
+  typedef uint64_t type;
+};
+
+// How the groups lie on the lanes.  Where a group is a power of two of whole lanes
+// (`span` of them), its best two come out of the lanes' own; else `sub` lanes, a power
+// of two, go over a group's experts in LDS.
 template <int NV>
 struct Groups {
-  int32_t per, sub, log_sub;
-  int32_t at[NV];
-  __device__ __forceinline__ void init(const RouteArgs& a, int lane) {
+  int32_t per, span, sub, log_sub;
+  float inv_per;
+  __device__ __forceinline__ void init(const RouteArgs& a) {
     per = a.E / a.groups;
-    log_sub = 6 - (32 - __clz(a.groups - 1));  // groups > 1
+    span = per % NV == 0 && ((per / NV) & (per / NV - 1)) == 0 ? per / NV : 0;
+    log_sub = span ? 31 - __clz(span) : 6 - (32 - __clz(a.groups - 1));  // groups > 1
     sub = 1 << log_sub;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      at[i] = (min((lane * NV + i) / per, a.groups - 1)) << log_sub;
+    inv_per = 1.f / (float)per;
   }
 };
 
-// Leaves in c (INT32_MIN: none) only the experts of the top_groups best groups.
-// `lds` is the wave's, for E values.
+// Leaves in x (INT32_MIN: none) only the experts of the top_groups best groups.
+// `lds` is the wave's, for E values; x is sorted and stays so where span > 0.
 template <int NV>
 __device__ __forceinline__ void keep_groups(const RouteArgs& a, const Groups<NV>& g,
-                                            int32_t (&c)[NV], int32_t* lds, int lane) {
-#pragma unroll
-  for (int i = 0; i < NV; ++i) lds[lane * NV + i] = c[i];
-  __builtin_amdgcn_wave_barrier();
+                                            Scored (&x)[NV], int32_t* lds, int lane) {
   const int32_t group = lane >> g.log_sub;
   int32_t b0 = INT32_MIN, b1 = INT32_MIN;  // the best two
-  if (group < a.groups)
-    for (int32_t i = lane & (g.sub - 1); i < g.per; i += g.sub) {
-      const int32_t v = lds[group * g.per + i];
-      b1 = max(b1, min(b0, v));
-      b0 = max(b0, v);
-    }
-  __builtin_amdgcn_wave_barrier();
-  for (int32_t o = 1; o < g.sub; o <<= 1) {
-    const int32_t o0 = __shfl_xor(b0, o, 64), o1 = __shfl_xor(b1, o, 64);
+  if (g.span) {
+    b0 = x[0].c;
+    if (NV > 1) b1 = x[NV > 1 ? 1 : 0].c;
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) lds[lane * NV + x[i].i] = x[i].c;
+    __builtin_amdgcn_wave_barrier();
+    if (group < a.groups)
+      for (int32_t i = lane & (g.sub - 1); i < g.per; i += g.sub) {
+        const int32_t v = lds[group * g.per + i];
+        b1 = max(b1, min(b0, v));
+        b0 = max(b0, v);
+      }
+    __builtin_amdgcn_wave_barrier();
+  }
+  const auto merge = [&](int32_t o0, int32_t o1) {
     b1 = max(max(b1, o1), min(b0, o0));
     b0 = max(b0, o0);
-  }
+  };
+  // lanes 1, 2, 4, 8 apart (mirrors do for 4 and 8: quads and halves are alike by then)
+  if (g.sub > 1) merge(dpp_or<0xb1, 0xf>(0, b0), dpp_or<0xb1, 0xf>(0, b1));
+  if (g.sub > 2) merge(dpp_or<0x4e, 0xf>(0, b0), dpp_or<0x4e, 0xf>(0, b1));
+  if (g.sub > 4) merge(dpp_or<0x141, 0xf>(0, b0), dpp_or<0x141, 0xf>(0, b1));
+  if (g.sub > 8) merge(dpp_or<0x140, 0xf>(0, b0), dpp_or<0x140, 0xf>(0, b1));
+  for (int32_t o = 16; o < g.sub; o <<= 1) merge(__shfl_xor(b0, o, 64), __shfl_xor(b1, o, 64));
   const int64_t score =
       b0 == INT32_MIN ? INT64_MIN : (int64_t)b0 + (a.group_best == 2 && b1 != INT32_MIN ? b1 : 0);
   int32_t rank = 0;
@@ -133,44 +180,58 @@ __device__ __forceinline__ void keep_groups(const RouteArgs& a, const Groups<NV>
                   (uint32_t)__builtin_amdgcn_readlane((int32_t)score, l));
     rank += other > score || (other == score && h < group);
   }
-  const uint64_t kept = __ballot(group < a.groups && b0 != INT32_MIN && rank < a.top_groups);
+  const bool stays = group < a.groups && b0 != INT32_MIN && rank < a.top_groups;
+  if (g.span) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) c[i] = (kept >> g.at[i]) & 1 ? c[i] : INT32_MIN;
+    for (int i = 0; i < NV; ++i) x[i].c = stays ? x[i].c : INT32_MIN;
+    return;
+  }
+  const uint64_t kept = __ballot(stays);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int32_t h = min(fdiv(lane * NV + x[i].i, g.per, g.inv_per), a.groups - 1);
+    x[i].c = (kept >> (h << g.log_sub)) & 1 ? x[i].c : INT32_MIN;
+  }
+  sort_lane<NV>(x);
 }
 
 // The choices of token t: writes expert and weight, enters them in the sets.
 template <int NV>
 __device__ __forceinline__ void choose(const RouteArgs& a, const Groups<NV>& g,
-                                       const int32_t (&bias)[NV], int32_t t, int32_t bit, int lane,
+                                       const int32_t* bias, int32_t t, int32_t bit, int lane,
                                        const uint32_t* table, int32_t* lds,
                                        unsigned long long* sets) {
-  int32_t s[NV], c[NV];
+  int32_t s[NV];
   uint32_t p[NV];
+  Scored x[NV];
   const int16_t* row = a.logits + (int64_t)t * a.ld;
 #pragma unroll
   for (int i = 0; i < NV; ++i) s[i] = lane * NV + i < a.E ? row[lane * NV + i] : kNoScore;
   probabilities<NV>(s, p, a.sigmoid, table);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) c[i] = s[i] == kNoScore ? INT32_MIN : (int32_t)p[i] + bias[i];
-  if (a.groups > 1) keep_groups<NV>(a, g, c, lds, lane);
+  for (int i = 0; i < NV; ++i) x[i] = {s[i] == kNoScore ? INT32_MIN : (int32_t)p[i] + bias[lane * NV + i], i};
+  sort_lane<NV>(x);
+  if (a.groups > 1) keep_groups<NV>(a, g, x, lds, lane);
 #pragma unroll
   for (int i = 0; i < NV; ++i) lds[lane * NV + i] = (int32_t)p[i];
   __builtin_amdgcn_wave_barrier();
+  // the lane's order, four bits an expert, so that the next one is a shift away
+  typedef typename Order<NV>::type order_t;
+  order_t order = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) order |= (order_t)x[i].i << (4 * i);
   int32_t expert = -1;  // lane j: choice j
   for (int32_t j = 0; j < a.top_k; ++j) {
-    int32_t m = c[0];
-#pragma unroll
-    for (int i = 1; i < NV; ++i) m = max(m, c[i]);
-    const int32_t best = scalar_max(m);
+    const int32_t best = scalar_max(x[0].c);
     if (best == INT32_MIN) break;
-    const int l = __ffsll((unsigned long long)__ballot(m == best)) - 1;
-    int32_t which = 0;
-#pragma unroll
-    for (int i = NV - 1; i >= 0; --i) which = c[i] == best ? i : which;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) c[i] = lane == l && which == i ? INT32_MIN : c[i];
-    const int32_t e = l * NV + __builtin_amdgcn_readlane(which, l);
+    const int l = __ffsll((unsigned long long)__ballot(x[0].c == best)) - 1;
+    const int32_t e = l * NV + (__builtin_amdgcn_readlane((int32_t)order, l) & (NV - 1));
     expert = lane == j ? e : expert;
+    const bool mine = lane == l;
+    order >>= mine ? 4 : 0;
+#pragma unroll
+    for (int i = 0; i + 1 < NV; ++i) x[i].c = mine ? x[i + 1].c : x[i].c;
+    x[NV - 1].c = mine ? INT32_MIN : x[NV - 1].c;
   }
   const uint32_t prob = expert >= 0 ? (uint32_t)lds[expert] : 0;
   __builtin_amdgcn_wave_barrier();
@@ -226,24 +287,28 @@ __device__ __forceinline__ void place(const RouteArgs& a, int32_t t0, const int3
   }
 }
 
+// Counts of a workgroup, in whole words.
+template <typename C>
+__host__ __device__ __forceinline__ int32_t count_stride(int32_t E) {
+  constexpr int W = 4 / sizeof(C);
+  return (E + W - 1) / W * W;
+}
+
 // Workgroup b has the sets b * per .. b * per + per - 1.
-template <int NV, bool ONE>
-__global__ __launch_bounds__(NT) void choose_kernel(RouteArgs a, int32_t* counts, int32_t per) {
+template <int NV, bool ONE, typename C>
+__global__ __launch_bounds__(NT) void choose_kernel(RouteArgs a, C* counts, int32_t per) {
   __shared__ uint32_t table[64];
   __shared__ unsigned long long sets[64 * NV];
-  __shared__ int32_t lds[WAVES][64 * NV];
+  __shared__ int32_t lds[WAVES][64 * NV], bias[64 * NV];
   __shared__ int32_t used;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   load_exp2(table);
   for (int32_t e = tid; e < 64 * NV; e += NT) sets[e] = 0;
-  int32_t bias[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i)
-    bias[i] = a.bias && lane * NV + i < a.E
-                  ? min(max(a.bias[lane * NV + i], -(1 << 30)), 1 << 30) : 0;
+  for (int32_t e = tid; e < 64 * NV; e += NT)
+    bias[e] = a.bias && e < a.E ? min(max(a.bias[e], -(1 << 30)), 1 << 30) : 0;
   Groups<NV> g;
-  if (a.groups > 1) g.init(a, lane);
+  if (a.groups > 1) g.init(a);
   __syncthreads();
   int32_t count = 0;  // of expert tid
   for (int32_t k = 0; k < per; ++k) {
@@ -262,7 +327,8 @@ __global__ __launch_bounds__(NT) void choose_kernel(RouteArgs a, int32_t* counts
     __syncthreads();
   }
   if (!ONE) {
-    if (tid < a.E) counts[(int64_t)blockIdx.x * a.E + tid] = count;
+    const int32_t ld = count_stride<C>(a.E);
+    if (tid < ld) counts[blockIdx.x * ld + tid] = (C)count;  // (0 behind the experts)
     return;
   }
   __syncthreads();
@@ -279,7 +345,8 @@ __global__ __launch_bounds__(NT) void choose_kernel(RouteArgs a, int32_t* counts
   for (int32_t i = used + tid; i < a.T * a.top_k; i += NT) a.rows[i] = -1;
 }
 
-__global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const int32_t* counts, int32_t per) {
+template <typename C>
+__global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const C* counts, int32_t per) {
   __shared__ unsigned long long sets[MAXE];
   __shared__ int32_t start[MAXE], before[MAXE];
   __shared__ int32_t used;
@@ -288,19 +355,31 @@ __global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const int32_t* c
   start[tid] = before[tid] = 0;
   sets[tid] = 0;
   __syncthreads();
-  // cols threads side by side take an expert each, NT / cols rows of counts at a time
-  const int32_t cols = a.E > 512 ? 1024 : a.E > 256 ? 512 : a.E > 128 ? 256 : a.E > 64 ? 128 : 64;
-  const int32_t e = tid & (cols - 1), step = NT / cols;
-  if (e < a.E) {
-    int32_t all = 0, mine = 0;
+  // cols threads side by side take a word of W counts each, NT / cols rows at a time
+  constexpr int W = 4 / sizeof(C);
+  const int32_t words = count_stride<C>(a.E) / W;
+  const int32_t lc = words > 1 ? 32 - __clz(words - 1) : 0, cols = 1 << lc;
+  const int32_t col = tid & (cols - 1), step = NT >> lc;
+  if (col < words) {
+    int32_t all[W], mine[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) all[i] = mine[i] = 0;
+    const uint32_t* c = (const uint32_t*)counts;
 #pragma unroll 8
-    for (int32_t k = tid / cols; k < nb; k += step) {
-      const int32_t c = counts[k * a.E + e];
-      all += c;
-      mine += k < b ? c : 0;
+    for (int32_t k = tid >> lc; k < nb; k += step) {
+      const uint32_t w = c[k * words + col];
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const int32_t v = W == 1 ? (int32_t)w : (int32_t)((w >> (32 / W * i)) & ((1u << (32 / W % 32)) - 1));
+        all[i] += v;
+        mine[i] += k < b ? v : 0;
+      }
     }
-    atomicAdd(&start[e], all);  // (whole numbers: in any order)
-    atomicAdd(&before[e], mine);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if (all[i]) atomicAdd(&start[col * W + i], all[i]);  // (whole numbers: in any order)
+      if (mine[i]) atomicAdd(&before[col * W + i], mine[i]);
+    }
   }
   __syncthreads();
   if (wave == 0) {
@@ -401,15 +480,15 @@ size_t route_workspace(int32_t T, int32_t E) {
   return blocks == 1 ? 0 : (size_t)blocks * E * sizeof(int32_t);
 }
 
-hipError_t launch_route(const RouteArgs& a, void* ws, hipStream_t s) {
+template <typename C>
+static hipError_t route_with(const RouteArgs& a, C* counts, hipStream_t s) {
   const int32_t per = route_sets(a.T), blocks = route_blocks(a.T);
-  int32_t* counts = (int32_t*)ws;
   const auto choose_with = [&](auto nv) {
     constexpr int NV = decltype(nv)::value;
-    if (blocks == 1)
-      hipLaunchKernelGGL((choose_kernel<NV, true>), dim3(1), dim3(NT), 0, s, a, counts, per);
-    else
-      hipLaunchKernelGGL((choose_kernel<NV, false>), dim3(blocks), dim3(NT), 0, s, a, counts, per);
+    if (blocks > 1)
+      hipLaunchKernelGGL((choose_kernel<NV, false, C>), dim3(blocks), dim3(NT), 0, s, a, counts, per);
+    else if constexpr (sizeof(C) == 1)
+      hipLaunchKernelGGL((choose_kernel<NV, true, C>), dim3(1), dim3(NT), 0, s, a, counts, per);
   };
   if (a.E <= 64) choose_with(IntC<1>{});
   else if (a.E <= 128) choose_with(IntC<2>{});
@@ -418,8 +497,15 @@ hipError_t launch_route(const RouteArgs& a, void* ws, hipStream_t s) {
   else choose_with(IntC<16>{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || blocks == 1) return e;
-  hipLaunchKernelGGL(place_kernel, dim3(blocks), dim3(NT), 0, s, a, counts, per);
+  hipLaunchKernelGGL((place_kernel<C>), dim3(blocks), dim3(NT), 0, s, a, counts, per);
   return hipGetLastError();
+}
+
+// A workgroup counts at most 64 sets of its tokens for an expert: in a byte up to 3
+// sets (16384 tokens of 256 experts: the counts that every workgroup reads are 64 KB,
+// 6.9 us a launch of place_kernel; in 32 bits 8.6).
+hipError_t launch_route(const RouteArgs& a, void* ws, hipStream_t s) {
+  return route_sets(a.T) * TB < 256 ? route_with(a, (uint8_t*)ws, s) : route_with(a, (int32_t*)ws, s);
 }
 
 bool combine_fits(const CombineArgs& a) {

@@ -140,6 +140,210 @@ __global__ __launch_bounds__(64 * WN * WM) void scaled_kernel(ScaledArgs a, uint
   }
 }
 
+// Few rows: the weights are what takes time.  A workgroup has 16 FI channels and 16 FJ
+// rows, its waves share K in steps of 128 (wave w: steps w, w + NW, ...), and each
+// wave streams its own weights through a ring of R steps in LDS that no other wave
+// touches, so no barrier holds the loads back; the rows come straight to registers.
+// The waves' sums meet in LDS at the end.
+template <int N>
+__device__ __forceinline__ void wait_vm() {  // all but the last N vector loads
+  static_assert(N < 64, "the counter's range");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+// A step's weights out of a slot, at LDS addresses a (first 64 inputs) and b, 16
+// channels each 2 KB; they are in the registers when it is done, so the slot may be
+// loaded again.  (Written as ordinary reads, the first slot's wait for the loads of
+// all slots: the compiler does not tell what lies between them.)
+template <int FI>
+__device__ __forceinline__ void read_step(v4i (&w)[2][FI], int a, int b) {
+  static_assert(FI == 1 || FI == 4, "the reads below");
+  if constexpr (FI == 1)
+    asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(w[0][0]), "=&v"(w[1][0])
+                 : "v"(a), "v"(b)
+                 : "memory");
+  else
+    asm volatile(
+        "ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:2048\n\t"
+        "ds_read_b128 %2, %8 offset:4096\n\tds_read_b128 %3, %8 offset:6144\n\t"
+        "ds_read_b128 %4, %9\n\tds_read_b128 %5, %9 offset:2048\n\t"
+        "ds_read_b128 %6, %9 offset:4096\n\tds_read_b128 %7, %9 offset:6144\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(w[0][0]), "=&v"(w[0][1]), "=&v"(w[0][2]), "=&v"(w[0][3]), "=&v"(w[1][0]),
+          "=&v"(w[1][1]), "=&v"(w[1][2]), "=&v"(w[1][3])
+        : "v"(a), "v"(b)
+        : "memory");
+}
+
+template <int R, typename F>
+__device__ __forceinline__ void steps_of(F f) {
+  static_assert(R == 2 || R == 4, "the steps below");
+  f(IntC<0>{});
+  f(IntC<1>{});
+  if constexpr (R == 4) {
+    f(IntC<2>{});
+    f(IntC<3>{});
+  }
+}
+
+typedef uint32_t u32x2a4 __attribute__((ext_vector_type(2), aligned(4)));
+
+template <int FI, int FJ, int NW, int R, int BYTES>
+__global__ __launch_bounds__(64 * NW) void stream_kernel(ScaledArgs a, uint32_t tiles_n) {
+  constexpr int TN = 16 * FI, TM = 16 * FJ, NT = 64 * NW, STEP = TN * KB, RING = R * STEP;
+  constexpr int WL = 2 * FI, XL = 2 * FJ;  // loads of a step: weights, rows
+  static_assert(FI * FJ * 1024 <= RING, "a wave's sums fit its ring");
+  static_assert(TN <= NT && TM <= NT, "a thread a constant");
+  __shared__ __attribute__((aligned(1024))) int8_t ring[NW * RING];
+  __shared__ Channel chan[TN];
+  __shared__ Token token[TM];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Tile tl = find_tile<TM, TN>(a, tiles_n, lane);
+  if (tl.m0 >= tl.m1) return;
+  const int32_t N = a.N, K = a.K, n0 = tl.n0;
+
+  // Row numbers, scales and constants first: loads return in order, and from the
+  // weights on a wait is for the step that it is meant for.  Scales and constants stay
+  // in registers until the sums are there.
+  int32_t xr[FJ], tr = min(tl.m0 + min(tid, TM - 1), tl.m1 - 1);
+#pragma unroll
+  for (int j = 0; j < FJ; ++j) xr[j] = min(tl.m0 + j * 16 + (lane & 15), tl.m1 - 1);
+  if (a.rows) {
+    tr = a.rows[tr];
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) xr[j] = a.rows[xr[j]];
+  }
+  const bool there = (uint64_t)(int64_t)tr < (uint64_t)a.x_rows;
+  tr = there ? tr : 0;
+  const int8_t* xp[FJ];
+#pragma unroll
+  for (int j = 0; j < FJ; ++j)
+    xp[j] = a.x + ((uint64_t)(int64_t)xr[j] < (uint64_t)a.x_rows ? (int64_t)xr[j] : 0) * K;
+  const int32_t S = a.x_scale[tr];
+  const int64_t cn = (int64_t)tl.e * N + min(n0 + min(tid, TN - 1), N - 1);
+  const int32_t mult = a.mult[a.nq == 1 ? 0 : cn], shift = a.shift[a.nq == 1 ? 0 : cn];
+  const int32_t some = (a.bias ? a.bias : a.mult)[a.bias ? cn : 0], bias = a.bias ? some : 0;
+
+  // weights: load i has rows 8 i + lane / 8, chunk lane % 8 of the swizzled line
+  const int8_t* wbase = a.w + ((int64_t)tl.e * N + n0) * K;
+  const uint32_t wrow = (uint32_t)(lane >> 3) * (uint32_t)K, wend = (uint32_t)(N - 1 - n0) * (uint32_t)K;
+  const int32_t wk = ((lane & 7) ^ ((lane >> 3) & 6)) * 16;
+  int8_t* mine = ring + wave * RING;
+  const int32_t nk = (K + KB - 1) / KB, ns = nk > wave ? (nk - wave - 1) / NW + 1 : 0;
+  const auto load_w = [&](int32_t s, int slot) {
+    // (past the row's end: any of its bytes, the rows' zeros meet them)
+    const uint32_t k = (uint32_t)min((wave + s * NW) * KB + wk, K - 16);
+#pragma unroll
+    for (int i = 0; i < WL; ++i)
+      load_lds16(wbase + (min(wrow + (uint32_t)(8 * i) * (uint32_t)K, wend) + k),
+                 mine + slot * STEP + i * 1024);
+  };
+  v4i x[R][FJ][2];
+  const int32_t xk = (lane >> 4) * 16;
+  const auto load_x = [&](int32_t s, v4i (&v)[FJ][2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t k = min((wave + s * NW) * KB + h * 64 + xk, K - 16);
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) v[j][h] = *(const v4i*)(xp[j] + k);
+    }
+  };
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    load_w(r, r);
+    load_x(r, x[r]);
+  }
+
+  const v4i zero = {0, 0, 0, 0};
+  v4i acc[FI][FJ];
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) acc[i][j] = zero;
+  int frag[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    frag[h] = (int)(uintptr_t)(__attribute__((address_space(3))) int8_t*)mine +
+              lds_chunk<8>(lane & 15, h * 4 + (lane >> 4));
+  }
+  const auto compute = [&](int slot, v4i (&v)[FJ][2]) {
+    v4i w[2][FI];
+    read_step<FI>(w, frag[0] + slot * STEP, frag[1] + slot * STEP);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < FI; ++i)
+#pragma unroll
+        for (int j = 0; j < FJ; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[h][i], v[j][h], acc[i][j], 0, 0, 0);
+  };
+  // Rounds of R steps without a branch.  All but the last load the next round's steps
+  // (which may lie past the end of the row: see load_w).
+  const int32_t rounds = max((ns + R - 1) / R, 1);
+  for (int32_t g = 0; g + 1 < rounds; ++g)
+    steps_of<R>([&](auto slot) {
+      constexpr int r = decltype(slot)::value;
+      wait_vm<(R - 1) * (WL + XL)>();
+      compute(r, x[r]);
+      load_w((g + 1) * R + r, r);
+      load_x((g + 1) * R + r, x[r]);
+    });
+  steps_of<R>([&](auto slot) {
+    constexpr int r = decltype(slot)::value;
+    const int32_t left = K - (wave + ((rounds - 1) * R + r) * NW) * KB;  // inputs from here on
+    wait_vm<(R - 1 - r) * (WL + XL)>();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) x[r][j][h] = h * 64 + xk < left ? x[r][j][h] : zero;
+    compute(r, x[r]);
+  });
+
+  // every wave's sums, each 16 x 16 tile 1 KB in the wave's ring
+#pragma unroll
+  for (int i = 0; i < FI; ++i)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) *(v4i*)(mine + (i * FJ + j) * 1024 + lane * 16) = acc[i][j];
+  if (tid < TN) chan[tid] = channel_of(mult, shift, bias);
+  // a row index that points nowhere is a row of zeros: no factor at all
+  if (tid < TM) token[tid] = token_of(there ? S : 0);
+  __syncthreads();
+  constexpr int32_t lim = BYTES == 1 ? 127 : 32767;
+  for (int f = wave; f < FI * FJ; f += NW) {
+    const int i = f / FJ, j = f % FJ;
+    v4i sum = zero;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) sum += *(const v4i*)(ring + w * RING + f * 1024 + lane * 16);
+    const int32_t t = j * 16 + (lane & 15), c = i * 16 + (lane >> 4) * 4;
+    const Token tk = token[t];
+    int32_t v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      v[r] = min(max(scaled<false>(sum[r], chan[c + r], tk), -lim), lim);
+    if (tl.m0 + t >= tl.m1 || n0 + c >= N) continue;
+    int8_t* dst = (int8_t*)a.y + ((int64_t)(tl.m0 + t) * N + n0 + c) * BYTES;
+    if (BYTES == 1)
+      *(uint32_t*)dst = pack4(v[0], v[1], v[2], v[3]);
+    else
+      *(u32x2a4*)dst = u32x2a4{__builtin_amdgcn_perm((uint32_t)v[1], (uint32_t)v[0], 0x05040100u),
+                               __builtin_amdgcn_perm((uint32_t)v[3], (uint32_t)v[2], 0x05040100u)};
+  }
+}
+
+template <int FI, int FJ, int NW, int R, int BYTES>
+hipError_t launch_stream(const ScaledArgs& a, hipStream_t s) {
+  constexpr int TN = 16 * FI, TM = 16 * FJ;
+  const uint32_t tiles_n = (uint32_t)((a.N + TN - 1) / TN);
+  const int64_t tiles_m =
+      a.offsets ? a.M / TM + (a.E < a.M ? a.E : a.M) : (a.M + TM - 1) / TM;
+  hipLaunchKernelGGL((stream_kernel<FI, FJ, NW, R, BYTES>), dim3((unsigned)(tiles_m * tiles_n)),
+                     dim3(64 * NW), 0, s, a, tiles_n);
+  return hipGetLastError();
+}
+
 template <int WN, int WM, int FI, int FJ, int BYTES>
 hipError_t launch_cfg(const ScaledArgs& a, hipStream_t s) {
   constexpr int TN = 16 * FI * WN, TM = 16 * FJ * WM;
@@ -158,11 +362,18 @@ hipError_t launch_cfg(const ScaledArgs& a, hipStream_t s) {
 
 template <int BYTES>
 hipError_t launch_bytes(const ScaledArgs& a, hipStream_t s) {
-  const int64_t size = a.M * a.N, unit = 65536;
-  if (a.M >= 192 * (int64_t)a.E && size > 128 * unit) return launch_cfg<4, 4, 4, 4, BYTES>(a, s);
-  if (a.M >= 64 * (int64_t)a.E && size >= 24 * unit) return launch_cfg<2, 4, 4, 2, BYTES>(a, s);
-  if (a.M <= 16 * (int64_t)a.E && a.E * (int64_t)((a.N + 255) / 256) >= 512)
-    return launch_cfg<4, 1, 4, 2, BYTES>(a, s);
+  const int64_t size = a.M * a.N, unit = 65536, E = a.E;
+  if (a.M <= 32 * E) {
+    const int64_t by64 = E * ((a.N + 63) / 64);
+    if (a.M <= 16) {
+      if (by64 >= 512) return launch_stream<4, 1, 4, 2, BYTES>(a, s);
+      return launch_stream<1, 1, 8, 4, BYTES>(a, s);
+    }
+    if (by64 >= 512) return launch_stream<4, 2, 4, 2, BYTES>(a, s);
+    return launch_stream<1, 2, 8, 4, BYTES>(a, s);
+  }
+  if (a.M >= 192 * E && size > 128 * unit) return launch_cfg<4, 4, 4, 4, BYTES>(a, s);
+  if (a.M >= 64 * E && size >= 24 * unit) return launch_cfg<2, 4, 4, 2, BYTES>(a, s);
   return launch_cfg<2, 2, 4, 2, BYTES>(a, s);
 }
 

@@ -99,16 +99,15 @@ __device__ __forceinline__ uint32_t exp2_q30(const uint32_t* table, uint32_t a) 
 }
 
 // floor((2^62 - 1) / D), exact for D in [2^30, 2^31]: one Newton step on the
-// hardware's FP64 reciprocal leaves an error below 2^-45 of a quotient of at most
-// 2^32, so its truncation is off by one at most and the remainder tells.
+// hardware's FP64 reciprocal leaves an error below 2^-13 of a quotient of at most
+// 2^32; taken off by 2^-10 its truncation is the quotient or one less (and below 2^32
+// for D = 2^30), and the remainder, in [0, 2 D), tells from its 32 bits.
 __device__ __forceinline__ uint32_t inverse_2p62(uint32_t D) {
   const double d = (double)D;
   double r = __builtin_amdgcn_rcp(d);
   r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
-  uint64_t q = (uint64_t)(0x1p62 * r);
-  const int64_t rem = (int64_t)((((uint64_t)1 << 62) - 1) - q * D);
-  q += rem < 0 ? -1 : (rem >= (int64_t)D ? 1 : 0);
-  return (uint32_t)q;
+  const uint32_t q = (uint32_t)__builtin_fma(0x1p62, r, -0x1p-10);
+  return q + (~(q * D) >= D);
 }
 
 __device__ __forceinline__ int32_t bit_length(uint64_t v) {

@@ -67,7 +67,8 @@ ROUTE = dict(top_k=4, groups=1, top_groups=1, group_best=2, sigmoid=0, renormali
     (dict(weight_shift=0), E_PARAM), (dict(weight_shift=63), E_PARAM),
     (dict(tokens=1 << 29), E_UNSUP), (dict(offsets=None), E_NULL), (dict(logits=None), E_NULL),
     (dict(expert=None), E_NULL), (dict(weight=None), E_NULL), (dict(rows=None), E_NULL),
-    (dict(slot=None), E_NULL), (dict(ws=None), E_WS), (dict(size=-1), E_WS)])
+    (dict(slot=None), E_NULL), (dict(ws=None), E_WS), (dict(size=-1), E_WS),
+    (dict(ws=FAKE + 4), E_PARAM)])
 def test_route_refusals(kw, code):
     f = dict(logits=FAKE, ld=64, bias=None, expert=FAKE, weight=FAKE, offsets=FAKE, rows=FAKE,
              slot=FAKE, tokens=200, experts=64)
