@@ -158,12 +158,19 @@ __device__ __forceinline__ void wait_vm() {  // all but the last N vector loads
 // all slots: the compiler does not tell what lies between them.)
 template <int FI>
 __device__ __forceinline__ void read_step(v4i (&w)[2][FI], int a, int b) {
-  static_assert(FI == 1 || FI == 4, "the reads below");
+  static_assert(FI == 1 || FI == 2 || FI == 4, "the reads below");
   if constexpr (FI == 1)
     asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)"
                  : "=&v"(w[0][0]), "=&v"(w[1][0])
                  : "v"(a), "v"(b)
                  : "memory");
+  else if constexpr (FI == 2)
+    asm volatile(
+        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:2048\n\t"
+        "ds_read_b128 %2, %5\n\tds_read_b128 %3, %5 offset:2048\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(w[0][0]), "=&v"(w[0][1]), "=&v"(w[1][0]), "=&v"(w[1][1])
+        : "v"(a), "v"(b)
+        : "memory");
   else
     asm volatile(
         "ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:2048\n\t"
@@ -229,13 +236,21 @@ __global__ __launch_bounds__(64 * NW) void stream_kernel(ScaledArgs a, uint32_t 
 
   // weights: load i has rows 8 i + lane / 8, chunk lane % 8 of the swizzled line
   const int8_t* wbase = a.w + ((int64_t)tl.e * N + n0) * K;
-  const uint32_t wrow = (uint32_t)(lane >> 3) * (uint32_t)K, wend = (uint32_t)(N - 1 - n0) * (uint32_t)K;
+  const uint32_t wrow = (uint32_t)(lane >> 3) * (uint32_t)K, 
+                 wend = (uint32_t)min(N - 1 - n0, TN - 1) * (uint32_t)K;  // the last row's
   const int32_t wk = ((lane & 7) ^ ((lane >> 3) & 6)) * 16;
   int8_t* mine = ring + wave * RING;
   const int32_t nk = (K + KB - 1) / KB, ns = nk > wave ? (nk - wave - 1) / NW + 1 : 0;
+  // Workgroups begin at different steps: where rows are a power of two of bytes apart,
+  // the same step of all of them would be in few memory channels.
+  const int32_t turn = K % KB == 0 ? (n0 / TN) % nk : 0;
+  const auto start_of = [&](int32_t s) {  // of the wave's step s
+    const int32_t k = wave + s * NW + turn;
+    return (k < nk ? k : k - nk) * KB;
+  };
   const auto load_w = [&](int32_t s, int slot) {
     // (past the row's end: any of its bytes, the rows' zeros meet them)
-    const uint32_t k = (uint32_t)min((wave + s * NW) * KB + wk, K - 16);
+    const uint32_t k = (uint32_t)min(start_of(s) + wk, K - 16);
 #pragma unroll
     for (int i = 0; i < WL; ++i)
       load_lds16(wbase + (min(wrow + (uint32_t)(8 * i) * (uint32_t)K, wend) + k),
@@ -246,7 +261,7 @@ __global__ __launch_bounds__(64 * NW) void stream_kernel(ScaledArgs a, uint32_t 
   const auto load_x = [&](int32_t s, v4i (&v)[FJ][2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int32_t k = min((wave + s * NW) * KB + h * 64 + xk, K - 16);
+      const int32_t k = min(start_of(s) + h * 64 + xk, K - 16);
 #pragma unroll
       for (int j = 0; j < FJ; ++j) v[j][h] = *(const v4i*)(xp[j] + k);
     }
@@ -360,17 +375,45 @@ hipError_t launch_cfg(const ScaledArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Which kernel, by the rows an expert has on average (what it really has is on the
+// device) and by how many workgroups c(TN, TM) = token tiles x channel tiles there
+// are.  Times in us, weights from memory, N x K:
+//   16 rows: up to 16 rows an expert, or as long as 32 channels a workgroup are at
+//     most 256 workgroups (32 rows of 4096 x 2048: 5.5, 32-row tiles 5.9; 64 rows:
+//     7.9 against 6.3).  64 channels from 1024 workgroups on (512 rows of 64 experts,
+//     2048 x 1024: 28.4, 32 channels 30.0; 16 rows of 16384 x 2048: 8.5 against
+//     8.2).  Few long rows take 16 channels and eight waves (1 row of 512 x 8192: 4.9
+//     against 6.7; of 1024 x 1024: 3.8 against 3.4).
+//   32 rows: up to 32 rows an expert, or up to 256 workgroups of 64 channels (512
+//     rows of 1024 x 1024: 6.2, 64-row tiles 7.7; 256 rows of 4096 x 2048: 13.8
+//     against 11.3).  32 channels up to 256 workgroups of them (64 rows of 4096 x
+//     2048: 6.3, 64 channels 7.5).
+//   64 rows: up to 64 rows an expert, or up to 512 workgroups (2048 rows of 1024 x
+//     1024: 10.4, tiles 14.0; 1024 rows of 4096 x 2048: 26.3 against 21.0).  Two waves
+//     from 1024 workgroups on (4096 rows of 64 experts, 2048 x 1024: 47.3, four 51.8;
+//     64 rows of 32768 x 4096: 37.4 against 36.5).
+//   More: tiles as of the linears grouped by expert, whose launch has both sides.
 template <int BYTES>
 hipError_t launch_bytes(const ScaledArgs& a, hipStream_t s) {
-  const int64_t size = a.M * a.N, unit = 65536, E = a.E;
-  if (a.M <= 32 * E) {
-    const int64_t by64 = E * ((a.N + 63) / 64);
-    if (a.M <= 16) {
-      if (by64 >= 512) return launch_stream<4, 1, 4, 2, BYTES>(a, s);
-      return launch_stream<1, 1, 8, 4, BYTES>(a, s);
-    }
-    if (by64 >= 512) return launch_stream<4, 2, 4, 2, BYTES>(a, s);
-    return launch_stream<1, 2, 8, 4, BYTES>(a, s);
+  // (every grid below 2^32 threads: the entry point holds (M / 64 + E) (N / 128 + 1)
+  // below 2^22, and the streams that are not limited here have M <= 64 E)
+  const int64_t E = a.E, size = a.M * a.N, unit = 65536;
+  const auto c = [&](int tn, int tm) {
+    const int64_t tiles = a.offsets ? a.M / tm + (E < a.M ? E : a.M) : (a.M + tm - 1) / tm;
+    return tiles * ((a.N + tn - 1) / tn);
+  };
+  if (a.M <= 16 * E || c(32, 16) <= 256) {
+    if (c(16, 16) <= 128 && a.K >= 2048) return launch_stream<1, 1, 8, 4, BYTES>(a, s);
+    if (c(64, 16) < 1024) return launch_stream<2, 1, 2, 4, BYTES>(a, s);
+    return launch_stream<4, 1, 2, 2, BYTES>(a, s);
+  }
+  if (a.M <= 32 * E || c(64, 32) <= 256) {
+    if (c(32, 32) <= 256) return launch_stream<2, 2, 2, 4, BYTES>(a, s);
+    return launch_stream<4, 2, 2, 2, BYTES>(a, s);
+  }
+  if (a.M <= 64 * E || c(64, 64) <= 512) {
+    if (c(64, 64) < 1024) return launch_stream<4, 4, 4, 2, BYTES>(a, s);
+    return launch_stream<4, 4, 2, 2, BYTES>(a, s);
   }
   if (a.M >= 192 * E && size > 128 * unit) return launch_cfg<4, 4, 4, 4, BYTES>(a, s);
   if (a.M >= 64 * E && size >= 24 * unit) return launch_cfg<2, 4, 4, 2, BYTES>(a, s);

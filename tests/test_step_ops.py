@@ -145,9 +145,12 @@ def test_linear_grouped(counts, N, K, bits):
     run_linear(c, M, bits, offsets, None, f"counts={counts} N={N} K={K} bits={bits}")
 
 
-# every tile: (rows an expert, experts, N, K) as the launch rule splits them
-TILES = [(200, 1, 48000, 64), (260, 2, 16784, 80), (70, 1, 24592, 64), (66, 3, 8208, 272),
-         (8, 1, 131104, 64), (3, 40, 3600, 80), (40, 2, 400, 128)]
+# every kernel that the launch rule chooses from, in its order: rows an expert, experts, N, K
+TILES = [(20, 1, 272, 2064), (7, 3, 96, 2304), (16, 1, 4000, 336), (5, 40, 112, 512),
+         (9, 1, 65552, 128), (3, 300, 272, 144), (30, 1, 4400, 272), (30, 1, 16400, 640),
+         (20, 9, 3600, 80), (60, 1, 16400, 144), (40, 6, 2576, 384), (50, 1, 65552, 80),
+         (45, 40, 1616, 128), (200, 1, 48000, 64), (260, 2, 16784, 80), (70, 1, 24592, 64),
+         (66, 3, 12304, 272), (70, 20, 1040, 128), (90, 17, 976, 48)]
 
 
 @pytest.mark.parametrize("per,E,N,K", TILES)
@@ -221,6 +224,25 @@ def test_linear_far_rows():
     plain.linear_scaled(x[at].cpu().numpy(), x_scale[at].cpu().numpy(), w[:, cols].cpu().numpy(),
                         None, np.array([1 << 30]), np.array([46]), offsets, None, 16, want)
     same(y[:, cols], want, "far rows")
+
+
+@pytest.mark.parametrize("K", [65536, 65552])
+def test_linear_far_channels(K):
+    """One matrix past 2^32 bytes."""
+    g = rng(11, K)
+    N = 66000
+    w = torch.randint(-127, 128, (N, K), dtype=torch.int8, device="cuda")
+    x = dev(g.integers(-127, 128, (3, K)).astype(np.int8))
+    x_scale = dev(np.array([1 << 14, 9000, 30000], np.int32))
+    mult, shift = (torch.full((1,), v, dtype=torch.int32, device="cuda") for v in (1 << 30, 46))
+    say(f"linear far channels K={K}")
+    y = ilw.ilw_linear_scaled(x, x_scale, w, None, mult, shift)
+    torch.cuda.synchronize()
+    cols = [0, 1, 63, 64, 40000, 65535, 65536, N - 17, N - 1]
+    want = np.zeros((3, len(cols)), np.int16)
+    plain.linear_scaled(x.cpu().numpy(), x_scale.cpu().numpy(), w[cols].cpu().numpy()[None], None,
+                        np.array([1 << 30]), np.array([46]), [0, 3], None, 16, want)
+    same(y[:, cols], want, "far channels")
 
 
 # --------------------------------------------------------------------- route
