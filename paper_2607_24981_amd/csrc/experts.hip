@@ -24,36 +24,6 @@ constexpr int TB = 64;     // tokens of a set
 constexpr int MAXB = 256;  // workgroups
 constexpr int MAXE = 1024;
 
-// Wave-wide results in every lane (scalar), by DPP within rows of 16 lanes and from
-// row to row: 6 vector instructions where exchanges through LDS take 6 round trips.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int32_t dpp_or(int32_t old, int32_t v) {
-  return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xf, false);
-}
-__device__ __forceinline__ int32_t scalar_max(int32_t v) {
-  v = max(v, dpp_or<0x111, 0xf>(INT32_MIN, v));  // row_shr 1, 2, 4, 8
-  v = max(v, dpp_or<0x112, 0xf>(INT32_MIN, v));
-  v = max(v, dpp_or<0x114, 0xf>(INT32_MIN, v));
-  v = max(v, dpp_or<0x118, 0xf>(INT32_MIN, v));
-  v = max(v, dpp_or<0x142, 0xa>(INT32_MIN, v));  // row_bcast 15, 31
-  v = max(v, dpp_or<0x143, 0xc>(INT32_MIN, v));
-  return __builtin_amdgcn_readlane(v, 63);
-}
-__device__ __forceinline__ uint32_t scalar_sum(uint32_t u) {
-  int32_t v = (int32_t)u;
-  v += dpp_or<0x111, 0xf>(0, v);
-  v += dpp_or<0x112, 0xf>(0, v);
-  v += dpp_or<0x114, 0xf>(0, v);
-  v += dpp_or<0x118, 0xf>(0, v);
-  v += dpp_or<0x142, 0xa>(0, v);
-  v += dpp_or<0x143, 0xc>(0, v);
-  return (uint32_t)__builtin_amdgcn_readlane(v, 63);
-}
-// Of values below 2^36.
-__device__ __forceinline__ uint64_t scalar_sum_u64(uint64_t v) {
-  return ((uint64_t)scalar_sum((uint32_t)(v >> 20)) << 20) + scalar_sum((uint32_t)v & 0xfffffu);
-}
-
 // Probabilities of a lane's NV scores in 2^-30.
 template <int NV>
 __device__ __forceinline__ void probabilities(const int32_t (&s)[NV], uint32_t (&p)[NV],

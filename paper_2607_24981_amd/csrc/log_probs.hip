@@ -9,15 +9,17 @@
 // each step.  So a row (or a part of one) stays in the registers of a workgroup, 8
 // scores to a 16-byte unit, and is read once.
 //
-// The best n: each of 64 groups of lanes has its largest score; the n-th largest of
-// these is at most the n-th largest of all, and what is not below it goes to a list
-// in LDS (about n + n^2/128 scores where the largest lie anywhere).  Each entry's
-// rank is the number of larger keys (score, then lower index).  Where ties overflow
-// the list, the n-th largest score is found by halving the range of scores, over the
+// The best n: each of 256 groups of lanes has its largest score; the n-th largest of
+// these is at most the n-th largest of all, and what is not below it goes to a list in
+// LDS (about n + n^2/512 scores where the largest lie anywhere).  Each entry's rank is
+// the number of larger keys (score, then lower index).  Where the list gets too long (ties),
+// the n-th largest score itself is found by halving the range of scores, over the
 // registers.
 //
 // A row with many scores and few rows beside it is cut in parts: their maxima and
-// best n in one launch, their sums in a second, a third joins them.
+// best n in one launch, their sums in a second, a third joins them.  (Joined by the
+// last workgroup of a row instead, with a fence and a count in each: 60 rows of 200003
+// scores 49 us.)
 #include "step_internal.h"
 
 namespace ilw {
@@ -32,6 +34,7 @@ __device__ __forceinline__ s16x2 pair(uint32_t w) { return __builtin_bit_cast(s1
 
 constexpr uint32_t NONE2 = 0x80008000u;  // two scores that are not to be had
 constexpr int32_t FAR = 31 * 64;         // weights from here on are 0
+constexpr int GROUPS = 256;
 constexpr int CAP = 1024;                // entries of the list
 constexpr int MAXN = 64;
 constexpr int MAXP = 64;  // parts of a row
@@ -70,6 +73,24 @@ __device__ __forceinline__ int32_t log_prob(int32_t s, int32_t top, int32_t lg) 
   return s == kNoScore ? kNoLogProb : (s - top) * 1024 - lg;
 }
 
+__device__ __forceinline__ uint32_t at_byte(const uint32_t* table, uint32_t offset) {
+  return *(const uint32_t*)((const int8_t*)table + offset);
+}
+// One 16-bit half of a (0: low) times one of b, added to c.
+template <int HA, int HB>
+__device__ __forceinline__ uint32_t mad_halves(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  if constexpr (HA == 0 && HB == 0)
+    asm("v_mad_u32_u16 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  else if constexpr (HA == 1 && HB == 0)
+    asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[1,0,0,0]" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  else if constexpr (HA == 0 && HB == 1)
+    asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[0,1,0,0]" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  else
+    asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[1,1,0,0]" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 // What a row's results are written from.
 __device__ __forceinline__ void write_given(const LogProbArgs& a, int64_t row, int32_t top,
                                             int32_t lg, int tid, int nt) {
@@ -98,12 +119,12 @@ enum { ALL = 0, BEST = 1, SUMS = 2 };
 
 template <int NT, int U, int MODE>
 __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs a, PartView ws, int32_t P) {
-  constexpr int WAVES = NT / 64, GL = NT / 64;  // lanes of a group
+  constexpr int WAVES = NT / 64, GL = NT / GROUPS;  // lanes of a group
   __shared__ uint32_t table[64];
-  __shared__ int32_t wave_top[WAVES], group_top[64];
+  __shared__ int32_t wave_top[WAVES], group_top[GROUPS];
   __shared__ unsigned long long wave_sum[WAVES][2];
   __shared__ unsigned long long list[MODE == SUMS ? 1 : CAP];
-  __shared__ int32_t count, bound, lg_shared, tally[WAVES];
+  __shared__ int32_t count, bound, lg_shared, tally[2][WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t row = blockIdx.x / (uint32_t)P;
   const int32_t part = (int32_t)(blockIdx.x - (uint32_t)row * (uint32_t)P);
@@ -135,8 +156,7 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs a, PartView w
 
   int32_t top;
   if (MODE == SUMS) {
-    top = kNoScore;
-    for (int32_t i = 0; i < P; ++i) top = max(top, ws.top[row * P + i]);
+    top = wave_max_i32(lane < P ? ws.top[row * P + lane] : kNoScore);  // (at most 64 parts)
     __syncthreads();
   } else {
     s16x2 m = {kNoScore, kNoScore};
@@ -160,75 +180,93 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs a, PartView w
   if (MODE != BEST) {
     uint64_t L = 0, B = 0;
     const uint32_t top2 = ((uint32_t)top & 0xffffu) * 0x10001u;
-    const auto add = [&](auto near) {
+    uint32_t blo = 0, bhi = 0;  // of the weights' low and high halves
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
-        __builtin_amdgcn_sched_barrier(0);  // (a unit's weights at a time: more would spill)
+    for (int k = 0; k < U; ++k) {
+      __builtin_amdgcn_sched_barrier(0);  // (a unit's weights at a time: more would spill)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          u16x2s d = __builtin_bit_cast(u16x2s, top2) - __builtin_bit_cast(u16x2s, pair(s[k][j]));
-          d = __builtin_elementwise_min(d, u16x2s{FAR, FAR});
-          if (decltype(near)::value) {
-            if ((s[k][j] & 0xffffu) == 0x8000u) d.x = FAR;
-            if ((s[k][j] >> 16) == 0x8000u) d.y = FAR;
-          }
-          const uint32_t a0 = d.x, a1 = d.y;
-          const uint32_t w0 = table[a0 & 63] >> (a0 >> 6), w1 = table[a1 & 63] >> (a1 >> 6);
-          L += w0 + w1;  // at most 2^31
-          B += (uint64_t)w0 * a0;
-          B += (uint64_t)w1 * a1;
-        }
+      for (int j = 0; j < 4; ++j) {
+        u16x2s d = __builtin_bit_cast(u16x2s, top2) - __builtin_bit_cast(u16x2s, pair(s[k][j]));
+        d = __builtin_elementwise_min(d, u16x2s{FAR, FAR});
+        const uint32_t a = __builtin_bit_cast(uint32_t, d),
+                       a4 = __builtin_bit_cast(uint32_t, d << u16x2s{2, 2});
+        const uint32_t w0 = at_byte(table, a4 & 0xfcu) >> ((a >> 6) & 31),
+                       w1 = at_byte(table, (a4 >> 16) & 0xffu) >> (a >> 22);
+        L += w0 + w1;  // at most 2^31
+        blo = mad_halves<0, 0>(w0, a, blo);
+        bhi = mad_halves<1, 0>(w0, a, bhi);
+        blo = mad_halves<0, 1>(w1, a, blo);
+        bhi = mad_halves<1, 1>(w1, a, bhi);
       }
-    };
-    if (top < kNoScore + FAR) add(Flag<true>{});  // -32768 itself would have a weight
-    else add(Flag<false>{});
+      // 32 terms below 2^16 FAR in blo, below 2^14 FAR + FAR in bhi
+      if (k % 4 == 3 || k == U - 1) {
+        B += blo + ((uint64_t)bhi << 16);
+        blo = bhi = 0;
+      }
+    }
+    if (top < kNoScore + FAR) {
+      // -32768 itself was given a weight, that of top + 32768
+      uint32_t none = 0;
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          none += ((s[k][j] & 0xffffu) == 0x8000u) + ((s[k][j] >> 16) == 0x8000u);
+      const uint32_t d = (uint32_t)(top - kNoScore), w = exp2_q30(table, d);
+      L -= (uint64_t)none * w;
+      B -= (uint64_t)none * w * d;
+    }
     L = wave_sum_u64(L);
     B = wave_sum_u64(B);
     if (lane == 0) wave_sum[wave][0] = L, wave_sum[wave][1] = B;
   }
 
   if (MODE != SUMS && n_top > 0) {
-    if (wave == 0) {  // the n-th largest of the groups' maxima
-      const int32_t g = group_top[lane];
-      int32_t rank = 0;
+    if (wave == 0) {  // the n-th largest of the groups' maxima, by halving
+      int32_t g[GROUPS / 64];
 #pragma unroll
-      for (int i = 0; i < 64; ++i) {
-        const int32_t o = __builtin_amdgcn_readlane(g, i);
-        rank += o > g || (o == g && i < lane);
+      for (int i = 0; i < GROUPS / 64; ++i) g[i] = group_top[lane + 64 * i];
+      int32_t lo = kNoScore + 1, hi = 32768;  // n groups or all reach lo, fewer hi
+      while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) >> 1;
+        int32_t c = 0;
+#pragma unroll
+        for (int i = 0; i < GROUPS / 64; ++i) c += __popcll(__ballot(g[i] >= mid));
+        if (c >= n_top) lo = mid;
+        else hi = mid;
       }
-      if (rank == n_top - 1) bound = max(g, kNoScore + 1);
+      if (lane == 0) bound = lo;
     }
     __syncthreads();
-    const auto collect = [&](int32_t least) {  // every score not below `least`
+    int32_t least = bound, ties = INT32_MIN, turn = 0;
+    for (;;) {
+      // every score not below `least`: few units have one
 #pragma unroll
       for (int k = 0; k < U; ++k) {
         s16x2 m = pair(s[k][0]);
 #pragma unroll
         for (int j = 1; j < 4; ++j) m = __builtin_elementwise_max(m, pair(s[k][j]));
         if (max((int32_t)m.x, (int32_t)m.y) < least) continue;
+        uint32_t hits = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int32_t v = (int16_t)(s[k][j >> 1] >> (16 * (j & 1)));
-          if (v < least) continue;
+        for (int j = 0; j < 8; ++j)
+          hits |= (uint32_t)((int32_t)(int16_t)(s[k][j >> 1] >> (16 * (j & 1))) >= least) << j;
+        while (hits) {
+          const int32_t j = __ffs(hits) - 1;
+          hits &= hits - 1;
+          const uint32_t w = j < 4 ? (j < 2 ? s[k][0] : s[k][1]) : (j < 6 ? s[k][2] : s[k][3]);
           const int32_t at = atomicAdd(&count, 1);
-          if (at < CAP) list[at] = key_of(v, v0 + (tid + k * NT) * 8 + j - off);
+          if (at < CAP)
+            list[at] = key_of((int16_t)(w >> (16 * (j & 1))), v0 + (tid + k * NT) * 8 + j - off);
         }
       }
-    };
-    collect(bound);
-    __syncthreads();
-    if (count > CAP) {
-      const auto total = [&](int32_t mine) {  // of the workgroup
-        mine = wave_sum_i32(mine);
-        __syncthreads();
-        if (lane == 0) tally[wave] = mine;
-        __syncthreads();
-        int32_t sum = 0;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) sum += tally[i];
-        return sum;
-      };
-      int32_t lo = kNoScore + 1, hi = 32768;  // at least n scores >= lo, fewer >= hi
+      __syncthreads();
+      // (A short row has fewer groups: 64 best of 400 scores, ranked among all 400, took
+      // 25 us, searched 12.)
+      if (ties != INT32_MIN || count <= (U == 1 ? 2 * MAXN : CAP)) break;
+      // More than that: the n-th largest score itself. At least n scores are not below
+      // lo, fewer than n are not below hi.
+      int32_t lo = kNoScore + 1, hi = 32768;
       while (hi - lo > 1) {
         const int32_t mid = (lo + hi) >> 1;
         int32_t c = 0;
@@ -236,14 +274,24 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs a, PartView w
         for (int k = 0; k < U; ++k)
 #pragma unroll
           for (int j = 0; j < 8; ++j) c += (int32_t)(int16_t)(s[k][j >> 1] >> (16 * (j & 1))) >= mid;
-        if (total(c) >= n_top) lo = mid;
+        c = (int32_t)scalar_sum((uint32_t)c);
+        turn ^= 1;  // (the other counts may still be read)
+        if (lane == 0) tally[turn][wave] = c;
+        __syncthreads();
+        c = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) c += tally[turn][i];
+        if (c >= n_top) lo = mid;
         else hi = mid;
       }
       __syncthreads();
       if (tid == 0) count = 0;
       __syncthreads();
-      if (hi <= 32767) collect(hi);
-      __syncthreads();
+      ties = lo;
+      least = hi;  // (32768: none)
+    }
+    if (ties != INT32_MIN) {
+      const int32_t lo = ties;
       // the first of those that equal the n-th largest, in the order of their index
       int32_t have = count;
 #pragma unroll 1
@@ -261,12 +309,12 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs a, PartView w
           before += lane >= o ? u : 0;
         }
         __syncthreads();
-        if (lane == 63) tally[wave] = before;
+        if (lane == 63) tally[0][wave] = before;
         __syncthreads();
         int32_t at = have + before - mine;
         for (int i = 0; i < WAVES; ++i) {
-          at += i < wave ? tally[i] : 0;
-          have += tally[i];
+          at += i < wave ? tally[0][i] : 0;
+          have += tally[0][i];
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -308,11 +356,16 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs a, PartView w
   }
   if (n_top == 0) return;
   const int32_t n = count;
-  for (int32_t i = tid; i < n; i += NT) {
-    const unsigned long long key = list[i];
+  // a key's rank is the number of larger ones: 16 lanes count them
+  for (int32_t i0 = 0; i0 < n; i0 += NT / 16) {
+    const int32_t i = i0 + tid / 16;
+    const unsigned long long key = i < n ? list[i] : 0;
     int32_t rank = 0;
-    for (int32_t j = 0; j < n; ++j) rank += list[j] > key;
-    if (rank >= n_top) continue;
+#pragma unroll 4
+    for (int32_t j = tid & 15; j < n; j += 16) rank += list[j] > key;
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) rank += __shfl_xor(rank, o, 64);
+    if (i >= n || rank >= n_top || (tid & 15)) continue;
     if (MODE == ALL) {
       a.top[row * n_top + rank] = key_index(key);
       a.top_lp[row * n_top + rank] = log_prob(key_score(key), top, lg);
@@ -330,65 +383,64 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs a, PartView w
   }
 }
 
-constexpr int JOIN = 256;
+constexpr int JOIN = 512;
 
+// The parts of a row joined.
 __global__ __launch_bounds__(JOIN) void log_probs_join_kernel(LogProbArgs a, PartView ws, int32_t P) {
   __shared__ unsigned long long keys[MAXP * MAXN];
+  __shared__ int32_t have;
   const int tid = threadIdx.x;
   const int64_t row = blockIdx.x;
   const int32_t n = a.n_top;
-  int32_t top = kNoScore;
-  uint64_t L = 0, B = 0;
-  for (int32_t i = 0; i < P; ++i) {
-    top = max(top, ws.top[row * P + i]);
-    L += ws.sums[2 * (row * P + i)];
-    B += ws.sums[2 * (row * P + i) + 1];
+  const int32_t lane = tid & 63;  // (at most 64 parts)
+  const int32_t top = wave_max_i32(lane < P ? ws.top[row * P + lane] : kNoScore);
+  const uint64_t L = wave_sum_u64(lane < P ? ws.sums[2 * (row * P + lane)] : 0),
+                 B = wave_sum_u64(lane < P ? ws.sums[2 * (row * P + lane) + 1] : 0);
+  int32_t mine = 0;
+  if (tid == 0) have = 0;
+  for (int32_t i = tid; i < P * n; i += JOIN) {
+    keys[i] = ws.keys[row * P * n + i];
+    mine += keys[i] != 0;
   }
-  for (int32_t i = tid; i < P * n; i += JOIN) keys[i] = ws.keys[row * P * n + i];
   const int32_t lg = L ? log2_q16(L) : 0;
   if (tid == 0) a.entropy[row] = L ? entropy_q16(lg, L, B) : 0;
   write_given(a, row, top, lg, tid, JOIN);
   __syncthreads();
-  // a key's rank: the larger keys of each part's sorted list (keys differ, but for 0)
-  for (int32_t i = tid; i < P * n; i += JOIN) {
-    const unsigned long long key = keys[i];
-    if (key == 0) continue;
+  if (mine) atomicAdd(&have, mine);
+  // a key's rank: the larger keys of each part's sorted list (keys differ, but for 0),
+  // four lanes a key
+  for (int32_t i0 = 0; i0 < P * n; i0 += JOIN / 4) {
+    const int32_t i = i0 + tid / 4;
+    const unsigned long long key = i < P * n ? keys[i] : 0;
     int32_t rank = 0;
-    for (int32_t p = 0; p < P && rank < n; ++p) {
-      int32_t lo = 0, hi = n;  // keys[p][lo - 1] > key >= keys[p][hi]
-      while (lo < hi) {
-        const int32_t mid = (lo + hi) >> 1;
-        if (keys[p * n + mid] > key) lo = mid + 1;
-        else hi = mid;
+    if (key)
+      for (int32_t p = tid & 3; p < P; p += 4) {
+        int32_t lo = 0, hi = n;  // keys[p][lo - 1] > key >= keys[p][hi]
+        while (lo < hi) {
+          const int32_t mid = (lo + hi) >> 1;
+          if (keys[p * n + mid] > key) lo = mid + 1;
+          else hi = mid;
+        }
+        rank += lo;
       }
-      rank += lo;
-    }
-    if (rank < n) {
-      a.top[row * n + rank] = key_index(key);
-      a.top_lp[row * n + rank] = log_prob(key_score(key), top, lg);
-    }
+    rank += __shfl_xor(rank, 1, 64);
+    rank += __shfl_xor(rank, 2, 64);
+    if (key == 0 || rank >= n || (tid & 3)) continue;
+    a.top[row * n + rank] = key_index(key);
+    a.top_lp[row * n + rank] = log_prob(key_score(key), top, lg);
   }
-  // fewer scores than n in all parts together
-  if (n > 0) {
-    int32_t have = 0;
-    for (int32_t i = 0; i < P * n && have < n; ++i) have += keys[i] != 0;
-    for (int32_t i = have + tid; i < n; i += JOIN) {
-      a.top[row * n + i] = -1;
-      a.top_lp[row * n + i] = kNoLogProb;
-    }
+  __syncthreads();
+  for (int32_t i = have + tid; i < n; i += JOIN) {  // fewer scores than n in all parts
+    a.top[row * n + i] = -1;
+    a.top_lp[row * n + i] = kNoLogProb;
   }
 }
 
-// Parts of a row: as many as its registers ask for, and more where rows are few.
+// Parts of a row: one up to the scores that a workgroup keeps.  (16 rows of 100003
+// scores, 20 best: 15 us; in 12 parts of two launches 29.)
 int32_t parts_of(const LogProbArgs& a) {
-  const int32_t most = 1024 * 14 * 8 - 16;  // scores a workgroup keeps
-  int64_t p = (a.V + most - 1) / most;
-  if (a.rows > 0 && a.rows < 64 && a.V > 65536) {
-    const int64_t want = 256 / a.rows, can = a.V / 8192;
-    const int64_t q = want < can ? want : can;
-    p = q > p ? q : p;
-  }
-  return (int32_t)(p < MAXP ? p : MAXP);
+  constexpr int32_t most = 1024 * 14 * 8 - 16, part = 1024 * 8 * 8 - 16;
+  return a.V <= most ? 1 : (a.V + part - 1) / part;
 }
 
 PartView carve(const LogProbArgs& a, int32_t P, void* ws) {
@@ -411,9 +463,8 @@ hipError_t launch_mode(const LogProbArgs& a, const PartView& v, int32_t P, hipSt
     hipLaunchKernelGGL((log_probs_kernel<NT, U, MODE>), grid, dim3(NT), 0, s, a, v, P);
     return hipGetLastError();
   };
-  if (MODE == ALL) {
-    if (units <= 64) return go(IntC<64>{}, IntC<1>{});
-    if (units <= 64 * 4) return go(IntC<64>{}, IntC<4>{});
+  if constexpr (MODE == ALL) {
+    if (units <= 256) return go(IntC<256>{}, IntC<1>{});
     if (units <= 256 * 4) return go(IntC<256>{}, IntC<4>{});
   }
   if (units <= 1024 * 2) return go(IntC<1024>{}, IntC<2>{});
