@@ -824,10 +824,12 @@ def ilw_quantize_rows(x, y=None, scale=None):
     M, K = x.shape
     if y is None:
         y = x.new_empty((M, K), dtype=torch.int8)
+    else:
+        _shape(y, (M, K), "y")
     if scale is None:
         scale = x.new_empty((M,), dtype=torch.int32)
-    _shape(y, (M, K), "y")
-    _shape(scale, (M,), "scale")
+    else:
+        _shape(scale, (M,), "scale")
     rc = lib().ilw_quantize_rows(at, _row_step(x), _at(y, torch.int8, "y", dev),
                                  _at(scale, torch.int32, "scale", dev), M, K, _raw_stream(dev))
     _check(rc, "ilw_quantize_rows")
@@ -864,7 +866,8 @@ def ilw_linear_scaled(x, x_scale, w, b, mult, shift, offsets=None, rows=None, bi
     dtype = torch.int16 if bits == 16 else torch.int8
     if y is None:
         y = x.new_empty((M, N), dtype=dtype)
-    _shape(y, (M, N), "y")
+    else:
+        _shape(y, (M, N), "y")
     rc = lib().ilw_linear_scaled(
         _at(x, torch.int8, "x", dev), R, _at(x_scale, torch.int32, "x_scale", dev),
         None if rows is None else _at(rows, torch.int32, "rows", dev),
@@ -895,21 +898,20 @@ def ilw_route(logits, top_k, bias=None, sigmoid=False, renormalize=True, groups=
     if workspace is None:
         need = L.ilw_route_workspace_bytes(T, E)
         workspace = torch.empty(need, dtype=torch.int8, device=logits.device) if need else None
-    # one allocation for the five results: offsets last, so that the others stay aligned
     n = T * top_k if top_k > 0 else 0
-    out = logits.new_empty((4 * n + E + 1,), dtype=torch.int32)
+    out = logits.new_empty((4, T, top_k if top_k > 0 else 0), dtype=torch.int32)
+    offsets = logits.new_empty((E + 1,), dtype=torch.int32)
     p = out.data_ptr()
     rp = RouteParams(top_k, groups, top_groups, group_best, sigmoid, renormalize, weight_mult,
                      weight_shift)
     rc = L.ilw_route(at, _row_step(logits),
                      None if bias is None else _at(bias, torch.int32, "bias", dev), p, p + 4 * n,
-                     p + 16 * n, p + 8 * n, p + 12 * n, T, E, rp,
+                     offsets.data_ptr(), p + 12 * n, p + 8 * n, T, E, rp,
                      None if workspace is None else _at(workspace, torch.int8, "workspace", dev),
                      0 if workspace is None else workspace.numel(), _raw_stream(dev))
     _check(rc, "ilw_route")
-    expert, weight, rows, slot, offsets = out.split([n, n, n, n, E + 1])
-    return Routing(expert.view(T, top_k), weight.view(T, top_k), offsets, rows,
-                   slot.view(T, top_k))
+    expert, weight, slot, rows = out.unbind()
+    return Routing(expert, weight, offsets, rows.view(-1), slot)
 
 
 def ilw_combine(v, slot, weight, mult, shift, skip=None, skip_mult=0, y=None):
@@ -925,10 +927,11 @@ def ilw_combine(v, slot, weight, mult, shift, skip=None, skip_mult=0, y=None):
     _shape(weight, (T, top_k), "weight")
     if skip is not None:
         _shape(skip, (T, N), "skip")
+    dt = v.dtype
     if y is None:
         y = v.new_empty((T, N))
-    _shape(y, (T, N), "y")
-    dt = v.dtype
+    else:
+        _shape(y, (T, N), "y")
     rc = lib().ilw_combine(
         _at(v, dt, "v", dev), 8 if dt is torch.int8 else 16, R,
         _at(slot, torch.int32, "slot", dev), _at(weight, torch.int32, "weight", dev),
