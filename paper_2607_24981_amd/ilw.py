@@ -804,34 +804,32 @@ def ilw_linear_grouped(x, w, offsets, b, mult, shift, rows=None, y=None):
     return y
 
 
-def _rows_at(t, dtype, name, device) -> int:
-    """Address of a matrix of that type on that device whose rows are contiguous."""
-    if not isinstance(t, _Tensor) or t.get_device() != device or t.dtype is not dtype or t.dim() != 2:
-        raise IlwError(f"{name} must be a matrix of {dtype} on cuda:{device}")
-    if t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1:
+def _rows_of(t, dtype, name):
+    """Device, address, rows, columns and row step of a matrix of that type on the
+    current device whose rows are contiguous."""
+    dev = _device(t, name)
+    if t.dtype is not dtype or t.dim() != 2:
+        raise IlwError(f"{name} must be a matrix of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+    (rows, cols), (step, inner) = t.shape, t.stride()
+    if inner != 1 and rows > 0 and cols > 1:
         raise IlwError(f"{name} must have contiguous rows")
-    return t.data_ptr()
-
-
-def _row_step(t) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return dev, t.data_ptr(), rows, cols, step if rows > 1 else cols
 
 
 def ilw_quantize_rows(x, y=None, scale=None):
     """x int16 [M, K] (its rows may be strided) -> y int8 [M, K], scale int32 [M]."""
-    dev = _device(x, "x")
-    at = _rows_at(x, torch.int16, "x", dev)
-    M, K = x.shape
+    dev, at, M, K, ld = _rows_of(x, torch.int16, "x")
     if y is None:
         y = x.new_empty((M, K), dtype=torch.int8)
     else:
         _shape(y, (M, K), "y")
+        _at(y, torch.int8, "y", dev)
     if scale is None:
         scale = x.new_empty((M,), dtype=torch.int32)
     else:
         _shape(scale, (M,), "scale")
-    rc = lib().ilw_quantize_rows(at, _row_step(x), _at(y, torch.int8, "y", dev),
-                                 _at(scale, torch.int32, "scale", dev), M, K, _raw_stream(dev))
+        _at(scale, torch.int32, "scale", dev)
+    rc = lib().ilw_quantize_rows(at, ld, y.data_ptr(), scale.data_ptr(), M, K, _raw_stream(dev))
     _check(rc, "ilw_quantize_rows")
     return y, scale
 
@@ -868,13 +866,14 @@ def ilw_linear_scaled(x, x_scale, w, b, mult, shift, offsets=None, rows=None, bi
         y = x.new_empty((M, N), dtype=dtype)
     else:
         _shape(y, (M, N), "y")
+        _at(y, dtype, "y", dev)
     rc = lib().ilw_linear_scaled(
         _at(x, torch.int8, "x", dev), R, _at(x_scale, torch.int32, "x_scale", dev),
         None if rows is None else _at(rows, torch.int32, "rows", dev),
         None if offsets is None else _at(offsets, torch.int32, "offsets", dev),
         _at(w, torch.int8, "w", dev), None if b is None else _at(b, torch.int32, "b", dev),
         Dyadic(_at(mult, torch.int32, "mult", dev), _at(shift, torch.int32, "shift", dev), n),
-        _at(y, dtype, "y", dev), bits, M, E, N, K, _raw_stream(dev))
+        y.data_ptr(), bits, M, E, N, K, _raw_stream(dev))
     _check(rc, "ilw_linear_scaled")
     return y
 
@@ -889,9 +888,7 @@ def ilw_route(logits, top_k, bias=None, sigmoid=False, renormalize=True, groups=
     bias int32 [E] in 2^-30 or None -> Routing.  Weights are in 2^-16 with the default
     factor.  offsets and rows go to ilw_linear_grouped and ilw_linear_scaled, slot and
     weight to ilw_combine."""
-    dev = _device(logits, "logits")
-    at = _rows_at(logits, torch.int16, "logits", dev)
-    T, E = logits.shape
+    dev, at, T, E, ld = _rows_of(logits, torch.int16, "logits")
     if bias is not None:
         _shape(bias, (E,), "bias")
     L = lib()
@@ -904,7 +901,7 @@ def ilw_route(logits, top_k, bias=None, sigmoid=False, renormalize=True, groups=
     p = out.data_ptr()
     rp = RouteParams(top_k, groups, top_groups, group_best, sigmoid, renormalize, weight_mult,
                      weight_shift)
-    rc = L.ilw_route(at, _row_step(logits),
+    rc = L.ilw_route(at, ld,
                      None if bias is None else _at(bias, torch.int32, "bias", dev), p, p + 4 * n,
                      offsets.data_ptr(), p + 12 * n, p + 8 * n, T, E, rp,
                      None if workspace is None else _at(workspace, torch.int8, "workspace", dev),
@@ -932,11 +929,12 @@ def ilw_combine(v, slot, weight, mult, shift, skip=None, skip_mult=0, y=None):
         y = v.new_empty((T, N))
     else:
         _shape(y, (T, N), "y")
+        _at(y, dt, "y", dev)
     rc = lib().ilw_combine(
         _at(v, dt, "v", dev), 8 if dt is torch.int8 else 16, R,
         _at(slot, torch.int32, "slot", dev), _at(weight, torch.int32, "weight", dev),
         None if skip is None else _at(skip, dt, "skip", dev), mult, skip_mult, shift,
-        _at(y, dt, "y", dev), T, top_k, N, _raw_stream(dev))
+        y.data_ptr(), T, top_k, N, _raw_stream(dev))
     _check(rc, "ilw_combine")
     return y
 
@@ -950,9 +948,7 @@ def ilw_log_probs(logits, given=None, top=0, workspace=None):
     had), given int32 [rows, n] token numbers or None -> LogProbs: log2 probabilities of
     the given tokens, the entropy in bits, the `top` best tokens and their log2
     probabilities, all but the token numbers in 2^-16."""
-    dev = _device(logits, "logits")
-    at = _rows_at(logits, torch.int16, "logits", dev)
-    rows, vocab = logits.shape
+    dev, at, rows, vocab, ld = _rows_of(logits, torch.int16, "logits")
     n = 0
     if given is not None:
         if given.dim() != 2 or given.shape[0] != rows:
@@ -965,10 +961,10 @@ def ilw_log_probs(logits, given=None, top=0, workspace=None):
             raise IlwError(f"ilw_log_probs_workspace_bytes: {last_error()}")
         workspace = torch.empty(need, dtype=torch.int8, device=logits.device) if need else None
     new = logits.new_empty
-    out = LogProbs(new((rows, n), dtype=torch.int32), new((rows,), dtype=torch.int32),
-                   new((rows, top), dtype=torch.int32), new((rows, top), dtype=torch.int32))
+    out = LogProbs(torch.empty_like(given) if n else new((rows, 0), dtype=torch.int32),
+                   new((rows,), dtype=torch.int32), *new((2, rows, top), dtype=torch.int32).unbind())
     rc = L.ilw_log_probs(
-        at, _row_step(logits), None if n == 0 else _at(given, torch.int32, "given", dev), n,
+        at, ld, None if n == 0 else _at(given, torch.int32, "given", dev), n,
         out.given.data_ptr(), out.entropy.data_ptr(), out.top.data_ptr(),
         out.top_log_prob.data_ptr(), rows, vocab, top,
         None if workspace is None else _at(workspace, torch.int8, "workspace", dev),
