@@ -11,18 +11,24 @@
 //                  all of them, which gives every expert's start, and places its
 //                  tokens 64 at a time: the rank of a token among the 64 that chose
 //                  an expert is a popcount of the expert's 64-bit set
-// 64 tokens or fewer are chosen and placed by one workgroup in one launch.  At most
-// MAXB workgroups share the tokens, so that the counts they all read stay few.  No
+// A few tokens are chosen and placed by one workgroup in one launch.  At most MAXB
+// workgroups share the tokens, so that the counts they all read stay few.  No
 // counter is shared between workgroups: the order does not depend on their timing.
 #include "step_internal.h"
 
 namespace ilw {
 namespace {
 
-constexpr int NT = 1024, WAVES = NT / 64;
-constexpr int TB = 64;     // tokens of a set
-constexpr int MAXB = 256;  // workgroups
+constexpr int SET = 64;    // tokens that place_kernel places at a time
+constexpr int MAXB = 256;  // workgroups of choose_kernel
 constexpr int MAXE = 1024;
+constexpr int NT = 1024;   // threads of place_kernel
+
+// How choose_kernel shares the tokens: `waves` a workgroup, which takes `sets` sets of
+// `tokens` tokens one after another and counts them together.
+struct Share {
+  int32_t waves, tokens, sets, blocks;
+};
 
 // Probabilities of a lane's NV scores in 2^-30.
 template <int NV>
@@ -241,11 +247,11 @@ __device__ __forceinline__ int32_t starts(int32_t* total, int32_t E, int lane) {
   return before;
 }
 
-// Places TB tokens from t0 on: start[e] is the row of the first that chose e.
+// Places 64 tokens from t0 on: start[e] is the row of the first that chose e.
 __device__ __forceinline__ void place(const RouteArgs& a, int32_t t0, const int32_t* start,
                                       const unsigned long long* sets) {
-  const int32_t n = min(TB, a.T - t0) * a.top_k;
-  for (int32_t i = threadIdx.x; i < n; i += NT) {
+  const int32_t n = min(SET, a.T - t0) * a.top_k;
+  for (int32_t i = threadIdx.x; i < n; i += blockDim.x) {
     const int64_t at = (int64_t)t0 * a.top_k + i;
     const int32_t e = a.expert[at], t = i / a.top_k;
     int32_t slot = -1;
@@ -264,64 +270,70 @@ __host__ __device__ __forceinline__ int32_t count_stride(int32_t E) {
   return (E + W - 1) / W * W;
 }
 
-// Workgroup b has the sets b * per .. b * per + per - 1.
-template <int NV, bool ONE, typename C>
-__global__ __launch_bounds__(NT) void choose_kernel(RouteArgs a, C* counts, int32_t per) {
+// Workgroup b has the sets b * sets .. b * sets + sets - 1.
+template <int NV, int WAVES, bool ONE, typename C>
+__global__ __launch_bounds__(64 * WAVES) void choose_kernel(RouteArgs a, C* counts, Share sh) {
+  constexpr int CNT = 64 * WAVES;
   __shared__ uint32_t table[64];
   __shared__ unsigned long long sets[64 * NV];
-  __shared__ int32_t lds[WAVES][64 * NV], bias[64 * NV];
+  __shared__ int32_t lds[WAVES][64 * NV], bias[64 * NV], count[ONE ? 1 : 64 * NV];
   __shared__ int32_t used;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   load_exp2(table);
-  for (int32_t e = tid; e < 64 * NV; e += NT) sets[e] = 0;
-  for (int32_t e = tid; e < 64 * NV; e += NT)
+  for (int32_t e = tid; e < 64 * NV; e += CNT) {
     bias[e] = a.bias && e < a.E ? min(max(a.bias[e], -(1 << 30)), 1 << 30) : 0;
+    sets[e] = 0;
+    if (!ONE) count[e] = 0;
+  }
   Groups<NV> g;
   if (a.groups > 1) g.init(a);
   __syncthreads();
-  int32_t count = 0;  // of expert tid
-  for (int32_t k = 0; k < per; ++k) {
-    const int64_t first = ((int64_t)blockIdx.x * per + k) * TB;
+  for (int32_t k = 0; k < sh.sets; ++k) {
+    const int64_t first = ((int64_t)blockIdx.x * sh.sets + k) * sh.tokens;
     if (first >= a.T && !ONE) break;
     const int32_t t0 = (int32_t)first;
-    const int32_t n = min(TB, a.T - t0);
+    const int32_t n = min(sh.tokens, a.T - t0);
     for (int32_t t = wave; t < n; t += WAVES)
       choose<NV>(a, g, bias, t0 + t, t, lane, table, lds[wave], sets);
     if (ONE) break;
     __syncthreads();
-    if (tid < 64 * NV) {
-      count += __popcll(sets[tid]);
-      sets[tid] = 0;
+    for (int32_t e = tid; e < 64 * NV; e += CNT) {
+      count[e] += __popcll(sets[e]);
+      sets[e] = 0;
     }
     __syncthreads();
   }
   if (!ONE) {
     const int32_t ld = count_stride<C>(a.E);
-    if (tid < ld) counts[blockIdx.x * ld + tid] = (C)count;  // (0 behind the experts)
+    for (int32_t e = tid; e < ld; e += CNT)  // (0 behind the experts)
+      counts[blockIdx.x * ld + e] = (C)count[e];
     return;
   }
   __syncthreads();
   int32_t* start = lds[0];
-  if (tid < a.E) start[tid] = __popcll(sets[tid]);
+  for (int32_t e = tid; e < a.E; e += CNT) start[e] = __popcll(sets[e]);
   __syncthreads();
   if (wave == 0) {
     const int32_t all = starts(start, a.E, lane);
     if (lane == 0) used = a.offsets[a.E] = all;
   }
   __syncthreads();
-  if (tid < a.E) a.offsets[tid] = start[tid];
+  for (int32_t e = tid; e < a.E; e += CNT) a.offsets[e] = start[e];
   place(a, 0, start, sets);  // (the workgroup's own stores, before barriers)
-  for (int32_t i = used + tid; i < a.T * a.top_k; i += NT) a.rows[i] = -1;
+  for (int32_t i = used + tid; i < a.T * a.top_k; i += CNT) a.rows[i] = -1;
 }
 
+// Workgroup b has the sets of 64 tokens b * per .. b * per + per - 1, whose counts are
+// `rows` of the nb rows.
 template <typename C>
-__global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const C* counts, int32_t per) {
+__global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const C* counts, int32_t per,
+                                                    int32_t rows, int32_t nb) {
   __shared__ unsigned long long sets[MAXE];
   __shared__ int32_t start[MAXE], before[MAXE];
   __shared__ int32_t used;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int32_t b = blockIdx.x, nb = gridDim.x;
+  const int32_t b = blockIdx.x;
   start[tid] = before[tid] = 0;
   sets[tid] = 0;
   __syncthreads();
@@ -342,7 +354,7 @@ __global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const C* counts,
       for (int i = 0; i < W; ++i) {
         const int32_t v = W == 1 ? (int32_t)w : (int32_t)((w >> (32 / W * i)) & ((1u << (32 / W % 32)) - 1));
         all[i] += v;
-        mine[i] += k < b ? v : 0;
+        mine[i] += k < b * rows ? v : 0;
       }
     }
 #pragma unroll
@@ -363,10 +375,10 @@ __global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const C* counts,
   }
   start[tid] += before[tid];
   for (int32_t k = 0; k < per; ++k) {
-    const int64_t first = ((int64_t)b * per + k) * TB;
+    const int64_t first = ((int64_t)b * per + k) * SET;
     if (first >= a.T) break;
     const int32_t t0 = (int32_t)first;
-    const int32_t n = min(TB, a.T - t0) * a.top_k;
+    const int32_t n = min(SET, a.T - t0) * a.top_k;
     __syncthreads();
     for (int32_t i = tid; i < n; i += NT) {
       const int32_t x = a.expert[(int64_t)t0 * a.top_k + i];
@@ -379,7 +391,7 @@ __global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const C* counts,
     sets[tid] = 0;
   }
   const int64_t all = (int64_t)a.T * a.top_k;
-  for (int64_t i = used + (int64_t)b * NT + tid; i < all; i += (int64_t)nb * NT) a.rows[i] = -1;
+  for (int64_t i = used + (int64_t)b * NT + tid; i < all; i += (int64_t)gridDim.x * NT) a.rows[i] = -1;
 }
 
 // ------------------------------------------------------------------- combine
@@ -435,30 +447,38 @@ int32_t combine_parts(const CombineArgs& a) { return (a.N * (a.bits / 8) / 16 + 
 
 }  // namespace
 
-// Sets of 64 tokens that a workgroup has.
-static int32_t route_sets(int32_t T) {
-  const int32_t sets = T > 0 ? (T - 1) / TB + 1 : 1;  // (no token: offsets of 0)
-  return (sets - 1) / MAXB + 1;
-}
-static int32_t route_blocks(int32_t T) {
-  const int32_t tokens = TB * route_sets(T);
-  return T > 0 ? (T - 1) / tokens + 1 : 1;
+// A wave a token as long as there are waves: a token takes 2 to 5 us one step after
+// the other, and a CU's waves share its issue slots.
+// One launch: 32 tokens of 64 experts 5.7 us, in two launches 6.4 (48: 7.2 and 6.7); of
+// 256 experts 24 tokens 9.8 and 9.2.  In sets of 64 as from 8192 tokens on, 526 tokens
+// of 256 experts took 23.9 us instead of 10.5.
+static Share share_of(int32_t T, int32_t E) {
+  if (T <= 32 && T * E <= 4096) return {16, SET, 1, 1};
+  if (T <= 4 * MAXB) return {4, 4, 1, (T + 3) / 4};
+  if (T <= 16 * MAXB) return {16, 16, 1, (T + 15) / 16};
+  if (T <= 32 * MAXB) return {16, 32, 1, (T + 31) / 32};
+  const int32_t sets = ((T - 1) / SET) / MAXB + 1, tokens = SET * sets;
+  return {16, SET, sets, (T - 1) / tokens + 1};
 }
 
 size_t route_workspace(int32_t T, int32_t E) {
-  const int32_t blocks = route_blocks(T);
+  const int32_t blocks = share_of(T, E).blocks;
   return blocks == 1 ? 0 : (size_t)blocks * E * sizeof(int32_t);
 }
 
 template <typename C>
-static hipError_t route_with(const RouteArgs& a, C* counts, hipStream_t s) {
-  const int32_t per = route_sets(a.T), blocks = route_blocks(a.T);
+static hipError_t route_with(const RouteArgs& a, C* counts, const Share& sh, hipStream_t s) {
+  const dim3 grid(sh.blocks);
   const auto choose_with = [&](auto nv) {
     constexpr int NV = decltype(nv)::value;
-    if (blocks > 1)
-      hipLaunchKernelGGL((choose_kernel<NV, false, C>), dim3(blocks), dim3(NT), 0, s, a, counts, per);
-    else if constexpr (sizeof(C) == 1)
-      hipLaunchKernelGGL((choose_kernel<NV, true, C>), dim3(1), dim3(NT), 0, s, a, counts, per);
+    if constexpr (sizeof(C) == 1) {
+      if (sh.blocks == 1)
+        hipLaunchKernelGGL((choose_kernel<NV, 16, true, C>), grid, dim3(1024), 0, s, a, counts, sh);
+      else if (sh.waves == 4)
+        hipLaunchKernelGGL((choose_kernel<NV, 4, false, C>), grid, dim3(256), 0, s, a, counts, sh);
+    }
+    if (sh.blocks > 1 && sh.waves == 16)
+      hipLaunchKernelGGL((choose_kernel<NV, 16, false, C>), grid, dim3(1024), 0, s, a, counts, sh);
   };
   if (a.E <= 64) choose_with(IntC<1>{});
   else if (a.E <= 128) choose_with(IntC<2>{});
@@ -466,16 +486,20 @@ static hipError_t route_with(const RouteArgs& a, C* counts, hipStream_t s) {
   else if (a.E <= 512) choose_with(IntC<8>{});
   else choose_with(IntC<16>{});
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || blocks == 1) return e;
-  hipLaunchKernelGGL((place_kernel<C>), dim3(blocks), dim3(NT), 0, s, a, counts, per);
+  if (e != hipSuccess || sh.blocks == 1) return e;
+  const int32_t rows = SET > sh.tokens ? SET / sh.tokens : 1;
+  hipLaunchKernelGGL((place_kernel<C>), dim3((sh.blocks - 1) / rows + 1), dim3(NT), 0, s, a, counts,
+                     sh.sets, rows, sh.blocks);
   return hipGetLastError();
 }
 
-// A workgroup counts at most 64 sets of its tokens for an expert: in a byte up to 3
-// sets (16384 tokens of 256 experts: the counts that every workgroup reads are 64 KB,
-// 6.9 us a launch of place_kernel; in 32 bits 8.6).
+// A workgroup's count of an expert is at most its tokens: in a byte up to 255 of them
+// (16384 tokens of 256 experts: the counts that every workgroup reads are 64 KB, 6.9 us
+// a launch of place_kernel; in 32 bits 8.6).
 hipError_t launch_route(const RouteArgs& a, void* ws, hipStream_t s) {
-  return route_sets(a.T) * TB < 256 ? route_with(a, (uint8_t*)ws, s) : route_with(a, (int32_t*)ws, s);
+  const Share sh = share_of(a.T, a.E);
+  return sh.sets * sh.tokens < 256 ? route_with(a, (uint8_t*)ws, sh, s)
+                                   : route_with(a, (int32_t*)ws, sh, s);
 }
 
 bool combine_fits(const CombineArgs& a) {

@@ -4,11 +4,12 @@
 //   y[m][n] = sat(floor((floor(acc F / 2^max(q - 4, 0)) + b + 8) / 16))
 // F = floor(X Y / 2^32) of the token's scale X = S 2^z in [2^31, 2^32) and the
 // channel's multiplier Y = mult 2^u in [2^30, 2^31), so that F is in [2^29, 2^31)
-// and keeps 29 bits or more whatever the scales are; q = shift + z + u - 18.  From
-// q = 36 on floor(acc F / 2^(q - 4)) is the product's high word shifted right: two
-// 32-bit high products, two adds, two shifts and a median a value.  Below, the
-// 64-bit product is shifted (q of a layer whose outputs use their bits is 37 and
-// more: acc of 13 bits, F of 30, outputs of 6).
+// and keeps 29 bits or more whatever the scales are; q = shift + z + u - 18.  A sum of
+// K products is below 2^14 K, so with e bits to spare, floor(acc F / 2^(q - 4)) is the
+// high word of (acc 2^e) F shifted right by q - 36 + e, from q = 36 - e on: two 32-bit
+// high products, two adds, three shifts and a median a value.  (q of a layer whose
+// outputs use their bits is 30 + the sums' bits - the outputs'.)  Below that the
+// 64-bit product is shifted.
 //
 // Tiles and their sums: expert_tiles.h.
 #include "step_internal.h"
@@ -40,12 +41,14 @@ __device__ __forceinline__ Token token_of(int32_t S) {
   r.X = S > 0 ? (uint32_t)S << r.z : 0;
   return r;
 }
-// One output before saturation; FAST: q >= 36.
+// Bits that a sum of K products leaves free.
+__device__ __forceinline__ int32_t spare_bits(int32_t K) { return max(__clz(K) - 15, 0); }
+// One output before saturation; FAST: q >= 36 - e, e the sums' spare bits.
 template <bool FAST>
-__device__ __forceinline__ int32_t scaled(int32_t acc, const Channel& c, const Token& t) {
+__device__ __forceinline__ int32_t scaled(int32_t acc, const Channel& c, const Token& t, int32_t e) {
   const int32_t F = (int32_t)__umulhi(t.X, c.Y);
   const int32_t s = c.q + t.z;
-  if (FAST) return ((__mulhi(acc, F) >> min(s - 32, 31)) + c.c) >> 4;
+  if (FAST) return ((__mulhi((int32_t)((uint32_t)acc << e), F) >> min(s - 32 + e, 31)) + c.c) >> 4;
   const int64_t v = (((int64_t)acc * F) >> min(max(s, 0), 63)) + c.c;
   return (int32_t)min(max(v >> 4, (int64_t)-65536), (int64_t)65536);
 }
@@ -93,6 +96,7 @@ __global__ __launch_bounds__(64 * WN * WM) void scaled_kernel(ScaledArgs a, uint
   p.run();
 
   // Epilogue: scale, transpose through LDS, 16-byte row chunks out.
+  const int32_t spare = spare_bits(a.K);
   uint32_t* so = (uint32_t*)sbuf;
   auto scale = [&](auto fast) {
     constexpr int32_t lim = BYTES == 1 ? 127 : 32767;
@@ -109,7 +113,7 @@ __global__ __launch_bounds__(64 * WN * WM) void scaled_kernel(ScaledArgs a, uint
         int32_t v[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          v[r] = min(max(scaled<decltype(fast)::value>(p.acc[i][j][r], ch[r], tok), -lim), lim);
+          v[r] = min(max(scaled<decltype(fast)::value>(p.acc[i][j][r], ch[r], tok, spare), -lim), lim);
         uint32_t* dst = so + (wm * WTM + j * 16 + (lane & 15)) * OSTR + (c * BYTES >> 2);
         if (BYTES == 1) {
           *dst = pack4(v[0], v[1], v[2], v[3]);
@@ -120,7 +124,7 @@ __global__ __launch_bounds__(64 * WN * WM) void scaled_kernel(ScaledArgs a, uint
       }
     }
   };
-  if (least_q + least_z >= 32) scale(Flag<true>{});
+  if (least_q + least_z >= 32 - spare) scale(Flag<true>{});
   else scale(Flag<false>{});
   lds_sync();
   constexpr int CH = TN * BYTES / 16;  // 16-byte chunks of a row
@@ -337,7 +341,7 @@ __global__ __launch_bounds__(64 * NW) void stream_kernel(ScaledArgs a, uint32_t 
     int32_t v[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      v[r] = min(max(scaled<false>(sum[r], chan[c + r], tk), -lim), lim);
+      v[r] = min(max(scaled<false>(sum[r], chan[c + r], tk, 0), -lim), lim);
     if (tl.m0 + t >= tl.m1 || n0 + c >= N) continue;
     int8_t* dst = (int8_t*)a.y + ((int64_t)(tl.m0 + t) * N + n0 + c) * BYTES;
     if (BYTES == 1)

@@ -75,7 +75,7 @@ def test_route_refusals(kw, code):
     rp = ilw.RouteParams(*[kw.get(k, v) for k, v in ROUTE.items()])
     f.update({k: v for k, v in kw.items() if k in f})
     need = ilw.lib().ilw_route_workspace_bytes(200, 64)
-    assert need > 0 and ilw.lib().ilw_route_workspace_bytes(64, 64) == 0
+    assert need > 0 and ilw.lib().ilw_route_workspace_bytes(32, 64) == 0
     check(ilw.lib().ilw_route(*f.values(), None if kw.get("rp") is False else ctypes.byref(rp),
                               kw.get("ws", FAKE), need + kw.get("size", 0), None), code)
 
