@@ -234,15 +234,9 @@ __device__ __forceinline__ void choose(const RouteArgs& a, const Groups<NV>& g,
 __device__ __forceinline__ int32_t starts(int32_t* total, int32_t E, int lane) {
   int32_t before = 0;
   for (int32_t e0 = 0; e0 < E; e0 += 64) {
-    const int32_t n = e0 + lane < E ? total[e0 + lane] : 0;
-    int32_t v = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int32_t u = __shfl_up(v, o, 64);
-      v += lane >= o ? u : 0;
-    }
+    const int32_t n = e0 + lane < E ? total[e0 + lane] : 0, v = wave_scan(n);
     if (e0 + lane < E) total[e0 + lane] = before + v - n;
-    before += __shfl(v, 63, 64);
+    before += __builtin_amdgcn_readlane(v, 63);
   }
   return before;
 }
@@ -251,9 +245,10 @@ __device__ __forceinline__ int32_t starts(int32_t* total, int32_t E, int lane) {
 __device__ __forceinline__ void place(const RouteArgs& a, int32_t t0, const int32_t* start,
                                       const unsigned long long* sets) {
   const int32_t n = min(SET, a.T - t0) * a.top_k;
+  const float inv_k = 1.f / (float)a.top_k;
   for (int32_t i = threadIdx.x; i < n; i += blockDim.x) {
     const int64_t at = (int64_t)t0 * a.top_k + i;
-    const int32_t e = a.expert[at], t = i / a.top_k;
+    const int32_t e = a.expert[at], t = fdiv(i, a.top_k, inv_k);
     int32_t slot = -1;
     if (e >= 0) {
       slot = start[e] + __popcll(sets[e] & (((unsigned long long)1 << t) - 1));
@@ -334,6 +329,20 @@ __global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const C* counts,
   __shared__ int32_t used;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t b = blockIdx.x;
+  const float inv_k = 1.f / (float)a.top_k;
+  static_assert(SET * 32 <= 2 * NT, "two choices a thread");
+  int32_t x[2];  // a set's choices: loaded, then entered in the sets
+  const auto load = [&](int32_t k) {
+    const int64_t first = ((int64_t)b * per + k) * SET;
+    const int32_t n = first < a.T ? min(SET, a.T - (int32_t)first) * a.top_k : 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i] = tid + i * NT < n ? a.expert[first * a.top_k + tid + i * NT] : -1;
+  };
+  const auto enter = [&]() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (x[i] >= 0) atomicOr(&sets[x[i]], 1ull << fdiv(tid + i * NT, a.top_k, inv_k));
+  };
   start[tid] = before[tid] = 0;
   sets[tid] = 0;
   __syncthreads();
@@ -363,6 +372,8 @@ __global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const C* counts,
       if (mine[i]) atomicAdd(&before[col * W + i], mine[i]);
     }
   }
+  load(0);
+  enter();
   __syncthreads();
   if (wave == 0) {
     const int32_t all = starts(start, a.E, lane);
@@ -378,17 +389,17 @@ __global__ __launch_bounds__(NT) void place_kernel(RouteArgs a, const C* counts,
     const int64_t first = ((int64_t)b * per + k) * SET;
     if (first >= a.T) break;
     const int32_t t0 = (int32_t)first;
-    const int32_t n = min(SET, a.T - t0) * a.top_k;
-    __syncthreads();
-    for (int32_t i = tid; i < n; i += NT) {
-      const int32_t x = a.expert[(int64_t)t0 * a.top_k + i];
-      if (x >= 0) atomicOr(&sets[x], 1ull << (i / a.top_k));
+    if (k > 0) {
+      load(k);
+      enter();
     }
     __syncthreads();
     place(a, t0, start, sets);
+    if (k + 1 == per) break;
     __syncthreads();
     start[tid] += __popcll(sets[tid]);
     sets[tid] = 0;
+    __syncthreads();
   }
   const int64_t all = (int64_t)a.T * a.top_k;
   for (int64_t i = used + (int64_t)b * NT + tid; i < all; i += (int64_t)gridDim.x * NT) a.rows[i] = -1;

@@ -125,15 +125,18 @@ __device__ __forceinline__ int32_t scalar_max(int32_t v) {
   v = max(v, dpp_or<0x143, 0xc>(INT32_MIN, v));
   return __builtin_amdgcn_readlane(v, 63);
 }
-__device__ __forceinline__ uint32_t scalar_sum(uint32_t u) {
-  int32_t v = (int32_t)u;
+// Sums of the lanes up to each one.
+__device__ __forceinline__ int32_t wave_scan(int32_t v) {
   v += dpp_or<0x111, 0xf>(0, v);
   v += dpp_or<0x112, 0xf>(0, v);
   v += dpp_or<0x114, 0xf>(0, v);
   v += dpp_or<0x118, 0xf>(0, v);
   v += dpp_or<0x142, 0xa>(0, v);
   v += dpp_or<0x143, 0xc>(0, v);
-  return (uint32_t)__builtin_amdgcn_readlane(v, 63);
+  return v;
+}
+__device__ __forceinline__ uint32_t scalar_sum(uint32_t u) {
+  return (uint32_t)__builtin_amdgcn_readlane(wave_scan((int32_t)u), 63);
 }
 // Of values below 2^36.
 __device__ __forceinline__ uint64_t scalar_sum_u64(uint64_t v) {
