@@ -9,6 +9,11 @@
 // each step.  So a row (or a part of one) stays in the registers of a workgroup, 8
 // scores to a 16-byte unit, and is read once.
 //
+// Bound: 200 rows of 100003 scores take 16.8 us without alternatives, 10.4 of them to
+// read (a workgroup a CU) and the rest for the weights and their sums, about ten vector
+// instructions a score that cannot begin before the last score is there.  (A table of
+// all 1985 weights saves the shifts and costs as much in LDS conflicts.)
+//
 // The best n: each of 256 groups of lanes has its largest score; the n-th largest of
 // these is at most the n-th largest of all, and what is not below it goes to a list in
 // LDS (about n + n^2/512 scores where the largest lie anywhere).  Each entry's rank is
@@ -76,21 +81,6 @@ __device__ __forceinline__ int32_t log_prob(int32_t s, int32_t top, int32_t lg) 
 __device__ __forceinline__ uint32_t at_byte(const uint32_t* table, uint32_t offset) {
   return *(const uint32_t*)((const int8_t*)table + offset);
 }
-// One 16-bit half of a (0: low) times one of b, added to c.
-template <int HA, int HB>
-__device__ __forceinline__ uint32_t mad_halves(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t r;
-  if constexpr (HA == 0 && HB == 0)
-    asm("v_mad_u32_u16 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  else if constexpr (HA == 1 && HB == 0)
-    asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[1,0,0,0]" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  else if constexpr (HA == 0 && HB == 1)
-    asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[0,1,0,0]" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  else
-    asm("v_mad_u32_u16 %0, %1, %2, %3 op_sel:[1,1,0,0]" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
-
 // What a row's results are written from.
 __device__ __forceinline__ void write_given(const LogProbArgs& a, int64_t row, int32_t top,
                                             int32_t lg, int tid, int nt) {
@@ -180,7 +170,6 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs a, PartView w
   if (MODE != BEST) {
     uint64_t L = 0, B = 0;
     const uint32_t top2 = ((uint32_t)top & 0xffffu) * 0x10001u;
-    uint32_t blo = 0, bhi = 0;  // of the weights' low and high halves
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       __builtin_amdgcn_sched_barrier(0);  // (a unit's weights at a time: more would spill)
@@ -193,15 +182,8 @@ __global__ __launch_bounds__(NT) void log_probs_kernel(LogProbArgs a, PartView w
         const uint32_t w0 = at_byte(table, a4 & 0xfcu) >> ((a >> 6) & 31),
                        w1 = at_byte(table, (a4 >> 16) & 0xffu) >> (a >> 22);
         L += w0 + w1;  // at most 2^31
-        blo = mad_halves<0, 0>(w0, a, blo);
-        bhi = mad_halves<1, 0>(w0, a, bhi);
-        blo = mad_halves<0, 1>(w1, a, blo);
-        bhi = mad_halves<1, 1>(w1, a, bhi);
-      }
-      // 32 terms below 2^16 FAR in blo, below 2^14 FAR + FAR in bhi
-      if (k % 4 == 3 || k == U - 1) {
-        B += blo + ((uint64_t)bhi << 16);
-        blo = bhi = 0;
+        B += (uint64_t)w0 * (a & 0xffffu);
+        B += (uint64_t)w1 * (a >> 16);
       }
     }
     if (top < kNoScore + FAR) {
