@@ -436,6 +436,15 @@ PartView carve(const LogProbArgs& a, int32_t P, void* ws) {
   return v;
 }
 
+// The workgroup, by the units of a row and by how many rows there are: threads keep 1
+// to 14 units.  Many rows take smaller workgroups, of which a CU has several, so that
+// one loads while another sums; few rows take more threads each.  In us, without
+// alternatives:
+//   2048 rows of 9000: 256 x 8 17.2, 512 x 4 20.3, 1024 x 2 41.7; 200 rows of 12000:
+//     256 x 8 6.2, 512 x 4 6.0, 1024 x 2 6.5.
+//   512 rows of 30000: 512 x 8 11.9, 1024 x 4 15.5; 200 rows of 32000, 8 best: 512 x 8
+//     10.1, 1024 x 4 9.8.
+//   400 rows of 50000: 512 x 14 15.9, 1024 x 8 20.9.
 template <int MODE>
 hipError_t launch_mode(const LogProbArgs& a, const PartView& v, int32_t P, hipStream_t s) {
   const dim3 grid((unsigned)(a.rows * P));
@@ -448,11 +457,14 @@ hipError_t launch_mode(const LogProbArgs& a, const PartView& v, int32_t P, hipSt
   if constexpr (MODE == ALL) {
     if (units <= 256) return go(IntC<256>{}, IntC<1>{});
     if (units <= 256 * 4) return go(IntC<256>{}, IntC<4>{});
+    if (units <= 256 * 8 && a.rows > 1024) return go(IntC<256>{}, IntC<8>{});
+    if (units <= 512 * 4) return go(IntC<512>{}, IntC<4>{});
+    if (units <= 512 * 8 && a.rows > 256) return go(IntC<512>{}, IntC<8>{});
+    if (units <= 1024 * 4) return go(IntC<1024>{}, IntC<4>{});
+    if (units <= 512 * 14 && a.rows > 256) return go(IntC<512>{}, IntC<14>{});
+    if (units > 1024 * 8) return go(IntC<1024>{}, IntC<14>{});
   }
-  if (units <= 1024 * 2) return go(IntC<1024>{}, IntC<2>{});
-  if (units <= 1024 * 4) return go(IntC<1024>{}, IntC<4>{});
-  if (units <= 1024 * 8) return go(IntC<1024>{}, IntC<8>{});
-  return go(IntC<1024>{}, IntC<14>{});
+  return go(IntC<1024>{}, IntC<8>{});  // (every part: see parts_of)
 }
 
 }  // namespace

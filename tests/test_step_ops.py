@@ -432,8 +432,8 @@ def run_log_probs(logits, given, n_top, what, pad=0, lead=0):
     return want
 
 
-VOCABS = [1, 2, 7, 8, 9, 63, 64, 100, 500, 512, 520, 2000, 2048, 2060, 5000, 8190, 16384, 16400,
-          32000, 50001, 65536, 70001, 114600, 114680, 131072, 200003]
+VOCABS = [1, 2, 7, 8, 9, 63, 64, 100, 500, 512, 520, 2032, 2048, 2060, 5000, 8176, 8190, 16368, 16384,
+          32000, 32752, 32770, 50001, 65520, 65536, 70001, 114672, 114673, 131040, 131072, 200003]
 
 
 @pytest.mark.parametrize("V", VOCABS)
@@ -485,7 +485,7 @@ def test_log_probs_long():
 
 def test_log_probs_many_rows():
     g = rng(2)
-    for rows, V in ((3000, 40), (700, 3000), (300, 20000)):
+    for rows, V in ((3000, 40), (700, 3000), (1030, 16368), (300, 20000), (257, 32752), (257, 57330)):
         x = np.rint(g.normal(0, 192, (rows, V))).astype(np.int16)
         run_log_probs(x, g.integers(0, V, (rows, 2)).astype(np.int32), 5, f"rows={rows} V={V}")
 
