@@ -410,41 +410,92 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int CT = 256, CWAVES = CT / 64;
 
-// A wave has 64 units of 16 bytes of a token's row.
-template <int BYTES>
-__global__ __launch_bounds__(CT) void combine_kernel(CombineArgs a, int32_t parts) {
-  constexpr int VALS = 16 / BYTES, lim = BYTES == 1 ? 127 : 32767;
-  const int lane = threadIdx.x & 63;
-  const int64_t wave = (int64_t)blockIdx.x * CWAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t t = wave / parts;
-  const int32_t unit = (int32_t)(wave - t * parts) * 64 + lane;
+// A thread has a unit of 16 bytes of a token's row.  WHOLE: rows are whole waves of
+// units, so that a wave's token, its slots and weights are scalars; else the units of
+// all tokens are numbered through and no lane idles (16384 tokens of 8 rows of 64 bytes
+// 6.7 us, 29 with a wave a token).  Four choices' rows are on their way at a time (8192
+// tokens of 8 rows of 2048 int8 values 34 us, one by one 37).
+//
+// Bound: bytes (8192 tokens of 8 rows of 2048 int16 values: 65 us, what 336 MB take to
+// copy).  int8 rows are summed in 32 bits where the wave's weights are below 2^18 (32
+// rows of them stay below 2^31): a 64-bit multiply-add a value takes longer than its
+// byte.
+template <int BYTES, bool WHOLE>
+__global__ __launch_bounds__(CT) void combine_kernel(CombineArgs a, int32_t units) {
+  constexpr int VALS = 16 / BYTES, lim = BYTES == 1 ? 127 : 32767, AT = 4;
+  int64_t t;
+  int32_t unit;
+  if (WHOLE) {
+    const int32_t parts = units / 64;
+    const int64_t wave = (int64_t)blockIdx.x * CWAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    t = wave / parts;
+    unit = (int32_t)(wave - t * parts) * 64 + (threadIdx.x & 63);
+  } else {
+    const uint32_t g = blockIdx.x * (uint32_t)CT + threadIdx.x, q = g / (uint32_t)units;
+    t = q;
+    unit = (int32_t)(g - q * (uint32_t)units);
+  }
+  if (t >= a.T) return;
   const int64_t ld = (int64_t)a.N * BYTES;
-  if (t >= a.T || unit * VALS >= a.N) return;
-  int64_t sum[VALS];
-#pragma unroll
-  for (int i = 0; i < VALS; ++i) sum[i] = 0;
+  const int8_t* v = (const int8_t*)a.v + unit * 16;
   const auto value = [](const u32x4& w, int i) {
     return BYTES == 1 ? (int32_t)(int8_t)(w[i >> 2] >> (8 * (i & 3)))
                       : (int32_t)(int16_t)(w[i >> 1] >> (16 * (i & 1)));
   };
-  for (int32_t j = 0; j < a.top_k; ++j) {
-    const int64_t s = a.slot[t * a.top_k + j];
-    const int32_t w = a.weight[t * a.top_k + j];
-    if ((uint64_t)s >= (uint64_t)a.v_rows) continue;
-    const u32x4 v = *(const u32x4*)((const int8_t*)a.v + s * ld + unit * 16);
-#pragma unroll
-    for (int i = 0; i < VALS; ++i) sum[i] += (int64_t)w * value(v, i);
-  }
-  u32x4 skip = {0, 0, 0, 0}, out;
+  u32x4 skip = {0, 0, 0, 0};
   if (a.skip) skip = *(const u32x4*)((const int8_t*)a.skip + t * ld + unit * 16);
+  const int32_t* slot = a.slot + t * a.top_k;
+  const int32_t* weight = a.weight + t * a.top_k;
   int32_t y[VALS];
+  const auto combine = [&](auto zero) {
+    decltype(zero) sum[VALS];
 #pragma unroll
-  for (int i = 0; i < VALS; ++i) {
-    const int64_t u = min(max((sum[i] + 128) >> 8, -(int64_t)INT32_MAX), (int64_t)INT32_MAX);
-    const int64_t v = (u * a.mult_a + (int64_t)value(skip, i) * a.mult_b +
-                       ((int64_t)1 << (a.shift - 1))) >> a.shift;
-    y[i] = (int32_t)min(max(v, (int64_t)-lim), (int64_t)lim);
+    for (int i = 0; i < VALS; ++i) sum[i] = 0;
+    if (a.v_rows > 0)
+      for (int32_t j0 = 0; j0 < a.top_k; j0 += AT) {
+        int64_t s[AT];
+        int32_t w[AT];
+        u32x4 x[AT];
+#pragma unroll
+        for (int i = 0; i < AT; ++i) {
+          const int32_t j = min(j0 + i, a.top_k - 1);
+          s[i] = slot[j];
+          w[i] = weight[j];
+          // (no such row: the first one, with no weight)
+          if ((uint64_t)s[i] >= (uint64_t)a.v_rows) s[i] = w[i] = 0;
+        }
+#pragma unroll
+        for (int i = 0; i < AT; ++i)
+          if (j0 + i < a.top_k) x[i] = *(const u32x4*)(v + s[i] * ld);
+#pragma unroll
+        for (int i = 0; i < AT; ++i) {
+          if (j0 + i >= a.top_k) break;
+#pragma unroll
+          for (int k = 0; k < VALS; ++k) {
+            if (sizeof(zero) == 4) sum[k] += __mul24(w[i], value(x[i], k));
+            else sum[k] += (int64_t)w[i] * value(x[i], k);
+          }
+        }
+      }
+#pragma unroll
+    for (int i = 0; i < VALS; ++i) {
+      const int64_t u = sizeof(zero) == 4
+                            ? ((int64_t)sum[i] + 128) >> 8
+                            : min(max(((int64_t)sum[i] + 128) >> 8, -(int64_t)INT32_MAX), (int64_t)INT32_MAX);
+      const int64_t r = (u * a.mult_a + (int64_t)value(skip, i) * a.mult_b +
+                         ((int64_t)1 << (a.shift - 1))) >> a.shift;
+      y[i] = (int32_t)min(max(r, (int64_t)-lim), (int64_t)lim);
+    }
+  };
+  if (BYTES == 1) {
+    uint32_t big = 0;
+    for (int32_t j = 0; j < a.top_k; ++j) big |= (uint32_t)(weight[j] ^ (weight[j] >> 31));
+    if (__all(big < 1u << 18)) combine((int32_t)0);
+    else combine((int64_t)0);
+  } else {
+    combine((int64_t)0);
   }
+  u32x4 out;
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     out[k] = BYTES == 1 ? pack4(y[4 * k % VALS], y[(4 * k + 1) % VALS], y[(4 * k + 2) % VALS],
@@ -454,7 +505,8 @@ __global__ __launch_bounds__(CT) void combine_kernel(CombineArgs a, int32_t part
   *(u32x4*)((int8_t*)a.y + t * ld + unit * 16) = out;
 }
 
-int32_t combine_parts(const CombineArgs& a) { return (a.N * (a.bits / 8) / 16 + 63) / 64; }
+// 16-byte units of a row.
+int32_t combine_units(const CombineArgs& a) { return a.N * (a.bits / 8) / 16; }
 
 }  // namespace
 
@@ -514,16 +566,19 @@ hipError_t launch_route(const RouteArgs& a, void* ws, hipStream_t s) {
 }
 
 bool combine_fits(const CombineArgs& a) {
-  return (a.T * combine_parts(a) + CWAVES - 1) / CWAVES < (int64_t)1 << 24;
+  return a.T * combine_units(a) < ((int64_t)1 << 32) - CT;
 }
 
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s) {
-  const int32_t parts = combine_parts(a);
-  const int64_t blocks = (a.T * parts + CWAVES - 1) / CWAVES;
-  if (a.bits == 8)
-    hipLaunchKernelGGL((combine_kernel<1>), dim3((unsigned)blocks), dim3(CT), 0, s, a, parts);
-  else
-    hipLaunchKernelGGL((combine_kernel<2>), dim3((unsigned)blocks), dim3(CT), 0, s, a, parts);
+  const int32_t units = combine_units(a);
+  const dim3 grid((unsigned)((a.T * units + CT - 1) / CT)), block(CT);
+  if (a.bits == 8) {
+    if (units % 64 == 0) hipLaunchKernelGGL((combine_kernel<1, true>), grid, block, 0, s, a, units);
+    else hipLaunchKernelGGL((combine_kernel<1, false>), grid, block, 0, s, a, units);
+  } else {
+    if (units % 64 == 0) hipLaunchKernelGGL((combine_kernel<2, true>), grid, block, 0, s, a, units);
+    else hipLaunchKernelGGL((combine_kernel<2, false>), grid, block, 0, s, a, units);
+  }
   return hipGetLastError();
 }
 

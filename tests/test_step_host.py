@@ -160,9 +160,9 @@ def test_plain_probabilities():
 
 
 # -------------------------------------------------------------- built kernels
-@pytest.mark.parametrize("name", ["quantize_kernel", "scaled_kernel", "choose_kernel",
-                                  "place_kernel", "combine_kernel", "log_probs_kernel",
-                                  "log_probs_join_kernel"])
+@pytest.mark.parametrize("name", ["quantize_kernel", "scaled_kernel", "stream_kernel",
+                                  "choose_kernel", "place_kernel", "combine_kernel",
+                                  "log_probs_kernel", "log_probs_join_kernel"])
 def test_no_private_memory(kernels, name):  # noqa: F811
     found = named(kernels, name)
     assert found

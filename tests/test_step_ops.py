@@ -400,9 +400,35 @@ def test_combine_extremes(dtype):
         y = ilw.ilw_combine(dev(v), dev(slot), dev(weight), ma, shift, skip=dev(skip), skip_mult=mb)
         torch.cuda.synchronize()
         same(y, plain.combine(v, slot, weight, ma, shift, skip, mb), f"{ma} {mb} {shift}")
+    # around the weights up to which a sum is held in fewer bits
+    v[:] = -lim - 1
+    weight[:] = np.array([[-(1 << 18)], [-(1 << 18) - 1], [1 << 18], [(1 << 18) - 1], [-(1 << 19)],
+                          [1 << 19]])
+    for pick in (slice(None), slice(0, 1), slice(1, 2), slice(3, 4), slice(4, 5)):
+        y = ilw.ilw_combine(dev(v), dev(slot[pick]), dev(weight[pick]), 1 << 10, 30)
+        torch.cuda.synchronize()
+        same(y, plain.combine(v, slot[pick], weight[pick], 1 << 10, 30, None, 0), f"{pick}")
     none = torch.empty(0, N, dtype=dev(v).dtype, device="cuda")
     y = ilw.ilw_combine(none, dev(slot), dev(weight), 1, 1, skip=dev(skip), skip_mult=2)
     same(y, plain.combine(v[:0], slot, weight, 1, 1, skip, 2), "no rows")
+
+
+@pytest.mark.parametrize("N", [16, 48, 1040, 1024, 8192 + 16])
+@pytest.mark.parametrize("dtype", [np.int8, np.int16])
+def test_combine_widths(dtype, N):
+    """Rows that end inside a wave; one, three and five choices; one and many tokens."""
+    say(f"combine N={N} {dtype.__name__}")
+    g = rng(N)
+    lim = np.iinfo(dtype).max
+    for T, top_k in ((1, 1), (7, 3), (131, 5)):
+        v = g.integers(-lim - 1, lim + 1, (T * top_k, N)).astype(dtype)
+        slot = g.integers(-2, T * top_k + 2, (T, top_k)).astype(np.int32)  # (a row twice, and none)
+        weight = g.integers(-(1 << 18), 1 << 18, (T, top_k)).astype(np.int32)
+        y = torch.full((T + 1, N), 55, dtype=dev(v).dtype, device="cuda")
+        ilw.ilw_combine(dev(v), dev(slot), dev(weight), 1 << 20, 30, y=y[:T])
+        torch.cuda.synchronize()
+        same(y[:T], plain.combine(v, slot, weight, 1 << 20, 30, None, 0), f"{T} {top_k}")
+        assert (y[T] == 55).all()
 
 
 def test_combine_far_rows():
