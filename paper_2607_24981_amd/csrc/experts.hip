@@ -566,7 +566,7 @@ hipError_t launch_route(const RouteArgs& a, void* ws, hipStream_t s) {
 }
 
 bool combine_fits(const CombineArgs& a) {
-  return a.T * combine_units(a) < ((int64_t)1 << 32) - CT;
+  return a.T < (((int64_t)1 << 32) - CT) / combine_units(a);
 }
 
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s) {

@@ -97,7 +97,8 @@ def test_workspace_refusals():
     (dict(mult_a=-2 ** 31), E_PARAM), (dict(mult_b=-2 ** 31), E_PARAM), (dict(shift=0), E_PARAM),
     (dict(shift=63), E_PARAM), (dict(v=None), E_NULL), (dict(slot=None), E_NULL),
     (dict(weight=None), E_NULL), (dict(y=None), E_NULL), (dict(v=FAKE + 8), E_PARAM),
-    (dict(skip=FAKE + 8), E_PARAM), (dict(y=FAKE + 4), E_PARAM), (dict(tokens=1 << 30), E_UNSUP)])
+    (dict(skip=FAKE + 8), E_PARAM), (dict(y=FAKE + 4), E_PARAM), (dict(tokens=1 << 31), E_UNSUP),
+    (dict(tokens=1 << 62), E_UNSUP)])
 def test_combine_refusals(kw, code):
     f = dict(v=FAKE, bits=8, v_rows=4, slot=FAKE, weight=FAKE, skip=FAKE, mult_a=5, mult_b=5,
              shift=20, y=FAKE, tokens=3, top_k=2, N=48)
