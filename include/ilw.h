@@ -562,8 +562,8 @@ int ilw_linear_grouped(const int8_t* x, int64_t x_rows, const int32_t* rows,
  * With A the largest magnitude of a row (-32768 counts as 32768):
  *   scale = max(1, ceil(2^14 A / 127));  y = floor((2^15 x + scale) / (2 scale))
  * in [-127, 127]: a code c stands for c * scale / 2^14 in units of x, as in the
- * paged cache above.  K a multiple of 16 in [16, 2^20]; x and y 16-byte aligned;
- * M == 0 is a no-op.  One launch; no workspace.  Calls whose M and K need more than
+ * paged cache above.  K a multiple of 16 in [16, 2^20]; x and y 16-byte aligned,
+ * y not aliasing x; M == 0 is a no-op.  One launch; no workspace.  Calls whose M and K need more than
  * a launch's 2^32 threads are refused with ILW_E_UNSUPPORTED.
  */
 int ilw_quantize_rows(const int16_t* x, int64_t ld, int8_t* y, int32_t* scale, int64_t M,

@@ -9,11 +9,12 @@
 // the rounding of R moves X / S by at most 2^15 1/2 2 / 2^40 (and 2^-17 of that for
 // the reciprocal's own error), so the sum is above the true value by less than
 // 2^17 / 2^40 = 2^-23, and (2 X + S) / (2 S), a multiple of 1 / (2 S) >= 2^-23.02
-// (S 2^e counted), meets no integer on the way.  x enters as x + 2^15, an unsigned 16-bit half of a
-// word, with the offset's product taken off the addend modulo 2^64.
+// (S 2^e counted), meets no integer on the way.  x enters as x + 2^15, an unsigned
+// 16-bit half of a word, with the offset's product taken off the addend modulo 2^64.
 //
-// Bound: bytes.  TPR lanes take a row, 16 values a unit, four units a lane in
-// registers (so that a row is read once up to 16384 values).
+// Bound: bytes (16000 rows of 4096 values: 35 us; 197 MB take 39 to copy).  TPR lanes
+// take a row, 16 values a unit, up to three units a lane (the widest: four) in
+// registers, so that a row is read once up to 16384 values.
 #include "step_internal.h"
 
 namespace ilw {
@@ -81,12 +82,12 @@ struct Codes {
   }
 };
 
-constexpr int UNITS = 4;  // a lane keeps
 constexpr int NT = 256;
 
 template <int TPR>
 __global__ __launch_bounds__(NT) void quantize_kernel(QuantizeArgs a) {
   constexpr int RPB = NT / TPR;  // rows a workgroup
+  constexpr int UNITS = TPR == NT ? 4 : 3;  // a lane keeps
   const int tid = threadIdx.x, t = tid % TPR;
   const int64_t m = (int64_t)blockIdx.x * RPB + tid / TPR;
   if (TPR < NT && m >= a.M) return;  // (no barrier below for these)
@@ -132,12 +133,16 @@ hipError_t launch(const QuantizeArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Lanes a row: as few as keep it in registers, and more where rows are few.
+// Lanes a row: as many as have two units each, or three where there is much to read.
+// In us, 4, 3 or 2 units a lane: 8000 rows of 256 values 3.9, 3.1 with 2; 40000 rows of
+// 640 16.5 with 3, 18.2 with 2, 8000 rows 5.4 and 5.5; 1000 rows of 1024 3.5 with 4, 2.5
+// with 1; 16000 rows of 4096 34.3 with 4, 31.6 with 1.  1 unit a lane leaves lanes idle
+// (40000 rows of 512: 17.2, 13.3 with 2).
 int lanes_of(const QuantizeArgs& a) {
-  const int32_t units = a.K / 16;
-  if (units <= 4 * UNITS) return 4;
-  if (units <= 16 * UNITS) return 16;
-  return units <= 64 * UNITS && a.M >= 1024 ? 64 : NT;
+  const int32_t units = a.K / 16, most = a.M >= ((int64_t)1 << 24) / a.K ? 3 : 2;
+  if (units <= 4 * most) return 4;
+  if (units <= 16 * most) return 16;
+  return units <= 64 * most ? 64 : NT;
 }
 
 }  // namespace

@@ -962,7 +962,8 @@ def ilw_log_probs(logits, given=None, top=0, workspace=None):
         workspace = torch.empty(need, dtype=torch.int8, device=logits.device) if need else None
     new = logits.new_empty
     out = LogProbs(torch.empty_like(given) if n else new((rows, 0), dtype=torch.int32),
-                   new((rows,), dtype=torch.int32), *new((2, rows, top), dtype=torch.int32).unbind())
+                   new((rows,), dtype=torch.int32),
+                   *new((2, rows, max(top, 0)), dtype=torch.int32).unbind())
     rc = L.ilw_log_probs(
         at, ld, None if n == 0 else _at(given, torch.int32, "given", dev), n,
         out.given.data_ptr(), out.entropy.data_ptr(), out.top.data_ptr(),

@@ -275,6 +275,7 @@ def test_binding_refuses():
         lambda: ilw.ilw_combine(x8, slot, slot.to(torch.int64), 1, 1),
         lambda: ilw.ilw_log_probs(x8), lambda: ilw.ilw_log_probs(x16, top=65),
         lambda: ilw.ilw_log_probs(x16, top=-1), lambda: ilw.ilw_log_probs(x16, given=s),
+        lambda: ilw.ilw_log_probs(x16, top=-1, workspace=x8.view(-1)),
         lambda: ilw.ilw_log_probs(x16, given=slot[:3]),
         lambda: ilw.ilw_log_probs(x16, given=slot.to(torch.int64)),
         lambda: ilw.ilw_log_probs(x16, given=z(4, 65, dtype=i32)),

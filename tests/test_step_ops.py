@@ -64,6 +64,37 @@ def test_quantize(M, K, pad):
     same(y, want[0], "y")
 
 
+@pytest.mark.parametrize("K", [16, 144, 560, 2336])
+def test_quantize_many_rows(K):
+    """Where three units a lane are in use: rows of 1, 9, 35 and 146 units."""
+    M = (1 << 24) // K + 5
+    say(f"quantize M={M} K={K}")
+    fewer = (np.arange(M) % 16).astype(np.int16)[:, None]
+    x = rng(K).integers(-32768, 32768, (M, K), dtype=np.int16) >> fewer
+    y, scale = ilw.ilw_quantize_rows(dev(x))
+    torch.cuda.synchronize()
+    some = np.r_[0:500, M // 2:M // 2 + 200, M - 500:M]
+    want = plain.quantize_rows(x[some])
+    same(scale[some], want[1], "scale")
+    same(y[some], want[0], "y")
+    most = np.abs(x.astype(np.int32)).max(1).astype(np.int64)
+    same(scale, np.maximum(1, -(-(most << 14) // 127)).astype(np.int32), "every scale")
+
+
+@pytest.mark.parametrize("M", [4, 700])
+@pytest.mark.parametrize("K", [112, 144, 528, 2032, 2064])
+def test_quantize_borders(M, K):
+    """Rows around what 4, 16 and 64 lanes hold in two units each."""
+    say(f"quantize M={M} K={K}")
+    fewer = (np.arange(M) % 16).astype(np.int16)[:, None]
+    x = rng(M, K).integers(-32768, 32768, (M, K), dtype=np.int16) >> fewer
+    y, scale = ilw.ilw_quantize_rows(dev(x))
+    torch.cuda.synchronize()
+    want = plain.quantize_rows(x)
+    same(scale, want[1], "scale")
+    same(y, want[0], "y")
+
+
 def test_quantize_every_magnitude():
     """Every largest magnitude there is, with the values whose codes are nearest to a
     tie, both signs."""
