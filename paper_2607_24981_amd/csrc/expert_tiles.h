@@ -6,8 +6,8 @@
 // (floor(M / TM) + E token tiles); a workgroup finds its expert from the offsets
 // by a wave-wide scan over the experts' tile counts and leaves if there is none.
 // A tile is WN x WM waves of FI x FJ MFMA tiles of 16 channels x 16 tokens.
-// Operands go from memory straight to LDS, 16 bytes a lane, in two buffers: the
-// loads of step k + 1 are in flight during the products of step k.  (Weights read
+// Operands go from memory straight to LDS, 16 bytes a lane, in S buffers: the loads of
+// the next S - 1 steps are in flight during the products of a step.  (Weights read
 // straight to registers where few rows use them: 34 us against 22, since a load
 // then takes 64 bytes of 16 rows where these take whole 128-byte lines.)
 #pragma once
@@ -80,11 +80,15 @@ __device__ __forceinline__ void load_lds16(const int8_t* src, int8_t* dst) {
                                    (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt 0
+template <int N = 0>
+__device__ __forceinline__ void wait_loads() {  // all but the last N vector loads
+  static_assert(N < 64, "the counter's range");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | ((N >> 4) << 14));
+}
 
 // The sums of a tile. Args has x, rows (or null), w, x_rows, N, K; the LDS buffer
-// holds 2 STAGE bytes, 1024-byte aligned.
-template <int WN, int WM, int FI, int FJ, bool KTAIL>
+// holds S STAGE bytes, 1024-byte aligned: S - 1 steps are loaded ahead.
+template <int WN, int WM, int FI, int FJ, bool KTAIL, int S = 2>
 struct TileProduct {
   static constexpr int WTN = 16 * FI, WTM = 16 * FJ, TN = WTN * WN, TM = WTM * WM,
                        NT = 64 * WN * WM;
@@ -100,7 +104,7 @@ struct TileProduct {
   int8_t* sbuf;
   v4i acc[FI][FJ];
 
-  // The addresses, and the first step's loads.
+  // The addresses, and the first steps' loads.
   template <typename Args>
   __device__ __forceinline__ void start(const Args& a, const Tile& tl, int8_t* lds, int tid) {
     K = a.K;
@@ -125,7 +129,9 @@ struct TileProduct {
         src[i] = a.x + xr * K;
       }
     }
-    load(0, 0);
+#pragma unroll
+    for (int i = 0; i + 1 < S; ++i)
+      if (i == 0 || i * KB < K) load(i, i);
   }
   __device__ __forceinline__ void load(int kt, int buf) {
     int8_t* dst = sbuf + buf * STAGE + wave * 1024;
@@ -142,7 +148,7 @@ struct TileProduct {
       }
     }
   }
-  // The first step's loads have arrived (and what the workgroup wrote to LDS).
+  // The first steps' loads have arrived (and what the workgroup wrote to LDS).
   __device__ __forceinline__ void ready() {
     wait_loads();
     lds_sync();
@@ -157,10 +163,13 @@ struct TileProduct {
     int frag_off[KB / 64];
 #pragma unroll
     for (int h = 0; h < KB / 64; ++h) frag_off[h] = lds_chunk<CPR>(lane & 15, h * 4 + (lane >> 4));
+    int ring = 0;
     for (int kt = 0; kt < nk; ++kt) {
-      if (kt + 1 < nk) load(kt + 1, (kt + 1) & 1);
-      const int8_t* sw = sbuf + (kt & 1) * STAGE + wn * WTN * KB;
-      const int8_t* sx = sbuf + (kt & 1) * STAGE + (TN + wm * WTM) * KB;
+      const int ahead = kt + S - 1, buf = S == 2 ? kt & 1 : ring;
+      if (ahead < nk) load(ahead, S == 2 ? ahead & 1 : buf == 0 ? S - 1 : buf - 1);
+      const int8_t* sw = sbuf + buf * STAGE + wn * WTN * KB;
+      const int8_t* sx = sbuf + buf * STAGE + (TN + wm * WTM) * KB;
+      ring = ring + 1 == S ? 0 : ring + 1;
 #pragma unroll
       for (int h = 0; h < KB / 64; ++h) {
         v4i fa[FI], fb[FJ];
@@ -174,7 +183,9 @@ struct TileProduct {
           for (int j = 0; j < FJ; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
       }
-      wait_loads();
+      // (the last steps, and one that is not loaded straight to LDS, count as none)
+      if (S > 2 && ahead < nk - KTAIL) wait_loads<(S - 2) * PT>();
+      else wait_loads();
       lds_sync();
     }
   }

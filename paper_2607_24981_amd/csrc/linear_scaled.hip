@@ -53,14 +53,14 @@ __device__ __forceinline__ int32_t scaled(int32_t acc, const Channel& c, const T
   return (int32_t)min(max(v >> 4, (int64_t)-65536), (int64_t)65536);
 }
 
-template <int WN, int WM, int FI, int FJ, int BYTES, bool KTAIL>
+template <int WN, int WM, int FI, int FJ, int BYTES, bool KTAIL, int S>
 __global__ __launch_bounds__(64 * WN * WM) void scaled_kernel(ScaledArgs a, uint32_t tiles_n) {
-  using Product = TileProduct<WN, WM, FI, FJ, KTAIL>;
+  using Product = TileProduct<WN, WM, FI, FJ, KTAIL, S>;
   constexpr int WTN = Product::WTN, WTM = Product::WTM, TN = Product::TN, TM = Product::TM,
                 NT = Product::NT, STAGE = Product::STAGE;
   constexpr int OSTR = TN * BYTES / 4 + 4;  // words per staged token row
   constexpr int SOUT = TM * OSTR * 4;
-  __shared__ __attribute__((aligned(1024))) int8_t sbuf[2 * STAGE > SOUT ? 2 * STAGE : SOUT];
+  __shared__ __attribute__((aligned(1024))) int8_t sbuf[S * STAGE > SOUT ? S * STAGE : SOUT];
   __shared__ Channel chan[TN];
   __shared__ Token token[TM];
   __shared__ int32_t least_q, least_z;
@@ -363,7 +363,7 @@ hipError_t launch_stream(const ScaledArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int WN, int WM, int FI, int FJ, int BYTES>
+template <int WN, int WM, int FI, int FJ, int BYTES, int S>
 hipError_t launch_cfg(const ScaledArgs& a, hipStream_t s) {
   constexpr int TN = 16 * FI * WN, TM = 16 * FJ * WM;
   const uint32_t tiles_n = (uint32_t)((a.N + TN - 1) / TN);
@@ -373,9 +373,9 @@ hipError_t launch_cfg(const ScaledArgs& a, hipStream_t s) {
   // and the one tile of 1024 threads has E <= M / 192
   const dim3 grid((unsigned)(tiles_m * tiles_n)), block(64 * WN * WM);
   if (a.K % KB == 0)
-    hipLaunchKernelGGL((scaled_kernel<WN, WM, FI, FJ, BYTES, false>), grid, block, 0, s, a, tiles_n);
+    hipLaunchKernelGGL((scaled_kernel<WN, WM, FI, FJ, BYTES, false, S>), grid, block, 0, s, a, tiles_n);
   else
-    hipLaunchKernelGGL((scaled_kernel<WN, WM, FI, FJ, BYTES, true>), grid, block, 0, s, a, tiles_n);
+    hipLaunchKernelGGL((scaled_kernel<WN, WM, FI, FJ, BYTES, true, S>), grid, block, 0, s, a, tiles_n);
   return hipGetLastError();
 }
 
@@ -396,7 +396,10 @@ hipError_t launch_cfg(const ScaledArgs& a, hipStream_t s) {
 //     1024: 10.4, tiles 14.0; 1024 rows of 4096 x 2048: 26.3 against 21.0).  Two waves
 //     from 1024 workgroups on (4096 rows of 64 experts, 2048 x 1024: 47.3, four 51.8;
 //     64 rows of 32768 x 4096: 37.4 against 36.5).
-//   More: tiles as of the linears grouped by expert, whose launch has both sides.
+//   More: tiles as of the linears grouped by expert, whose launch has both sides.  Up to
+//     256 of 128 x 128, one a CU, load three steps ahead (4096 rows of 1024 x 8192: 48.4,
+//     one step 66; 700 rows of 4096 x 4096: 26.8 and 29.8); more of them load one, so
+//     that a CU has two (2048 rows of 4096 x 4096: 44.6, three steps 59.6).
 template <int BYTES>
 hipError_t launch_bytes(const ScaledArgs& a, hipStream_t s) {
   // (every grid below 2^32 threads: the entry point holds (M / 64 + E) (N / 128 + 1)
@@ -419,9 +422,12 @@ hipError_t launch_bytes(const ScaledArgs& a, hipStream_t s) {
     if (c(64, 64) < 1024) return launch_stream<4, 4, 4, 2, BYTES>(a, s);
     return launch_stream<4, 4, 2, 2, BYTES>(a, s);
   }
-  if (a.M >= 192 * E && size > 128 * unit) return launch_cfg<4, 4, 4, 4, BYTES>(a, s);
-  if (a.M >= 64 * E && size >= 24 * unit) return launch_cfg<2, 4, 4, 2, BYTES>(a, s);
-  return launch_cfg<2, 2, 4, 2, BYTES>(a, s);
+  if (a.M >= 192 * E && size > 128 * unit) return launch_cfg<4, 4, 4, 4, BYTES, 2>(a, s);
+  if (a.M >= 64 * E && size >= 24 * unit) {
+    if (c(128, 128) <= 256) return launch_cfg<2, 4, 4, 2, BYTES, 4>(a, s);
+    return launch_cfg<2, 4, 4, 2, BYTES, 2>(a, s);
+  }
+  return launch_cfg<2, 2, 4, 2, BYTES, 2>(a, s);
 }
 
 }  // namespace

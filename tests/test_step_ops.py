@@ -184,6 +184,17 @@ TILES = [(20, 1, 272, 2064), (7, 3, 96, 2304), (16, 1, 4000, 336), (5, 40, 112, 
          (66, 3, 12304, 272), (70, 20, 1040, 128), (90, 17, 976, 48)]
 
 
+@pytest.mark.parametrize("K", [16, 112, 128, 144, 256, 272, 384, 400, 512, 528, 640, 1040])
+@pytest.mark.parametrize("M,N,E", [(1024, 2064, 1), (1100, 2064, 9), (4096, 1040, 1)])
+def test_linear_steps(M, N, E, K):
+    """1 to 9 steps, whole ones and partial last ones, of tiles that load three steps
+    ahead and (the last sizes) one."""
+    g = rng(M, N, K)
+    c = linear_case(g, M, N, K, E, M, 8, False, True)
+    offsets = [0, M] if E == 1 else np.r_[0, np.sort(g.integers(0, M, E - 1)), M]
+    run_linear(c, M, 8, offsets, None, f"M={M} N={N} E={E} K={K}", dense=E == 1)
+
+
 @pytest.mark.parametrize("per,E,N,K", TILES)
 @pytest.mark.parametrize("bits", [8, 16])
 def test_linear_tiles(per, E, N, K, bits):
