@@ -417,15 +417,15 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int CT = 256, CWAVES = CT / 64;
 
 // A thread has a unit of 16 bytes of a token's row.  WHOLE: rows are whole waves of
-// units, so that a wave's token, its slots and weights are scalars; else the units of
-// all tokens are numbered through and no lane idles (16384 tokens of 8 rows of 64 bytes
-// 6.7 us, 29 with a wave a token).  Four choices' rows are on their way at a time (8192
-// tokens of 8 rows of 2048 int8 values 34 us, one by one 37).
+// units, so that a wave's token, its slots and weights are scalars (8192 tokens of 8 rows
+// of 2048 int8 values 33.5 us, numbered through 39.3); else the units of all tokens are
+// numbered through and no lane idles (16384 tokens of 8 rows of 64 bytes 6.7 us, 29 with
+// a wave a token).  Four choices' rows are on their way at a time.
 //
 // Bound: bytes (8192 tokens of 8 rows of 2048 int16 values: 65 us, what 336 MB take to
 // copy).  int8 rows are summed in 32 bits where the wave's weights are below 2^18 (32
 // rows of them stay below 2^31): a 64-bit multiply-add a value takes longer than its
-// byte.
+// byte (16384 tokens of 4 rows of 1024 values 24.4 us so, 22.5 in 32 bits).
 template <int BYTES, bool WHOLE>
 __global__ __launch_bounds__(CT) void combine_kernel(CombineArgs a, int32_t units) {
   constexpr int VALS = 16 / BYTES, lim = BYTES == 1 ? 127 : 32767, AT = 4;
@@ -520,7 +520,8 @@ int32_t combine_units(const CombineArgs& a) { return a.N * (a.bits / 8) / 16; }
 // the other, and a CU's waves share its issue slots.
 // One launch: 32 tokens of 64 experts 5.7 us, in two launches 6.4 (48: 7.2 and 6.7); of
 // 256 experts 24 tokens 9.8 and 9.2.  In sets of 64 as from 8192 tokens on, 526 tokens
-// of 256 experts took 23.9 us instead of 10.5.
+// of 256 experts took 23.9 us instead of 10.5; 16384 in 512 workgroups of 32, whose
+// counts take longer to read, 30.2 instead of 26.6.
 static Share share_of(int32_t T, int32_t E) {
   if (T <= 32 && T * E <= 4096) return {16, SET, 1, 1};
   if (T <= 4 * MAXB) return {4, 4, 1, (T + 3) / 4};
