@@ -11,6 +11,7 @@ from __future__ import annotations
 import collections
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch
@@ -187,6 +188,18 @@ def last_error() -> str:
 def _check(rc: int, name: str):
     if rc != 0:
         raise IlwError(f"{name} failed with status {rc}: {last_error()}")
+
+
+_PACK = [None] + [struct.Struct(f"{n}i").pack for n in range(1, 17)]
+
+
+def _int32(call, *values):
+    """The values as the C entry's 32-bit numbers lie in memory; refuses what does not fit
+    (ctypes would pass its low bits: 5 << 30 as 1 << 30).  0.1 us a call."""
+    try:
+        return _PACK[len(values)](*values)
+    except struct.error:
+        raise IlwError(f"{call}: not all of {values} are whole numbers of 32 bits") from None
 
 
 def _stream():
@@ -819,6 +832,7 @@ def _rows_of(t, dtype, name):
 def ilw_quantize_rows(x, y=None, scale=None):
     """x int16 [M, K] (its rows may be strided) -> y int8 [M, K], scale int32 [M]."""
     dev, at, M, K, ld = _rows_of(x, torch.int16, "x")
+    _int32("ilw_quantize_rows", K)
     if y is None:
         y = x.new_empty((M, K), dtype=torch.int8)
     else:
@@ -861,6 +875,7 @@ def ilw_linear_scaled(x, x_scale, w, b, mult, shift, offsets=None, rows=None, bi
         raise IlwError(f"mult and shift have {n} and {shift.numel()} entries")
     if bits != 16 and bits != 8:
         raise IlwError(f"bits must be 8 or 16, got {bits}")
+    _int32("ilw_linear_scaled", E, N, K, n)
     dtype = torch.int16 if bits == 16 else torch.int8
     if y is None:
         y = x.new_empty((M, N), dtype=dtype)
@@ -891,6 +906,10 @@ def ilw_route(logits, top_k, bias=None, sigmoid=False, renormalize=True, groups=
     dev, at, T, E, ld = _rows_of(logits, torch.int16, "logits")
     if bias is not None:
         _shape(bias, (E,), "bias")
+    _int32("ilw_route", T, E)
+    rp = RouteParams.from_buffer_copy(_int32(
+        "ilw_route", top_k, groups, top_groups, group_best, sigmoid, renormalize, weight_mult,
+        weight_shift))
     L = lib()
     if workspace is None:
         need = L.ilw_route_workspace_bytes(T, E)
@@ -899,8 +918,6 @@ def ilw_route(logits, top_k, bias=None, sigmoid=False, renormalize=True, groups=
     out = logits.new_empty((4, T, top_k if top_k > 0 else 0), dtype=torch.int32)
     offsets = logits.new_empty((E + 1,), dtype=torch.int32)
     p = out.data_ptr()
-    rp = RouteParams(top_k, groups, top_groups, group_best, sigmoid, renormalize, weight_mult,
-                     weight_shift)
     rc = L.ilw_route(at, ld,
                      None if bias is None else _at(bias, torch.int32, "bias", dev), p, p + 4 * n,
                      offsets.data_ptr(), p + 12 * n, p + 8 * n, T, E, rp,
@@ -921,6 +938,7 @@ def ilw_combine(v, slot, weight, mult, shift, skip=None, skip_mult=0, y=None):
     (R, N), (T, top_k) = v.shape, slot.shape
     if v.dtype is not torch.int8 and v.dtype is not torch.int16:
         raise IlwError(f"v must be int8 or int16, got {v.dtype}")
+    _int32("ilw_combine", top_k, N, mult, skip_mult, shift)
     _shape(weight, (T, top_k), "weight")
     if skip is not None:
         _shape(skip, (T, N), "skip")
@@ -954,6 +972,7 @@ def ilw_log_probs(logits, given=None, top=0, workspace=None):
         if given.dim() != 2 or given.shape[0] != rows:
             raise IlwError(f"given must be [{rows}, tokens], got {tuple(given.shape)}")
         n = given.shape[1]
+    _int32("ilw_log_probs", vocab, n, top)
     L = lib()
     if workspace is None:
         need = L.ilw_log_probs_workspace_bytes(rows, vocab, top)
