@@ -240,6 +240,7 @@ def ilw_linear(x, w, b, mult, shift, y=None):
 
 def ilw_shiftmax(x, I0, k_inter=16, k_out=8, m_p=4, s_d=-1, y=None):
     rows, cols = x.shape
+    _int32("ilw_shiftmax", I0, k_inter, k_out, m_p, s_d)
     if y is None:
         y = torch.empty_like(x)
     rc = lib().ilw_shiftmax(_dev(x, torch.int8, "x"), _dev(y, torch.int8, "y"), rows, cols,
@@ -249,6 +250,7 @@ def ilw_shiftmax(x, I0, k_inter=16, k_out=8, m_p=4, s_d=-1, y=None):
 
 
 def ilw_sdshiftgelu(x, I0, out_mult, out_shift, k_inter=16, k_out=8, y=None):
+    _int32("ilw_sdshiftgelu", I0, k_inter, k_out, out_mult, out_shift)
     if y is None:
         y = torch.empty_like(x)
     rc = lib().ilw_sdshiftgelu(_dev(x, torch.int8, "x"), _dev(y, torch.int8, "y"), x.numel(),
@@ -259,6 +261,7 @@ def ilw_sdshiftgelu(x, I0, out_mult, out_shift, k_inter=16, k_out=8, y=None):
 
 def ilw_int_layernorm(x, beta, mult, shift, newton_iters=10, y=None):
     C = x.shape[-1]
+    _int32("ilw_int_layernorm", newton_iters)
     if y is None:
         y = torch.empty_like(x)
     rc = lib().ilw_int_layernorm(_dev(x, torch.int8, "x"), _dev(y, torch.int8, "y"),
@@ -269,6 +272,7 @@ def ilw_int_layernorm(x, beta, mult, shift, newton_iters=10, y=None):
 
 
 def ilw_residual_add(a, b, mult_a, mult_b, shift, y=None):
+    _int32("ilw_residual_add", mult_a, mult_b, shift)
     if y is None:
         y = torch.empty_like(a)
     rc = lib().ilw_residual_add(_dev(a, torch.int8, "a"), _dev(b, torch.int8, "b"),
@@ -279,10 +283,10 @@ def ilw_residual_add(a, b, mult_a, mult_b, shift, y=None):
 
 
 def attn_params(p: dict) -> AttnParams:
-    return AttnParams(int(p["score_mult"]), int(p["score_shift"]), int(p["smax_I0"]),
-                      int(p.get("smax_k_inter", 16)), int(p.get("smax_k_out", 8)),
-                      int(p.get("smax_m_p", 4)), int(p.get("smax_s_d", -1)),
-                      int(p["pv_mult"]), int(p["pv_shift"]))
+    return AttnParams.from_buffer_copy(_int32(
+        "attention parameters", int(p["score_mult"]), int(p["score_shift"]), int(p["smax_I0"]),
+        int(p.get("smax_k_inter", 16)), int(p.get("smax_k_out", 8)), int(p.get("smax_m_p", 4)),
+        int(p.get("smax_s_d", -1)), int(p["pv_mult"]), int(p["pv_shift"])))
 
 
 def ilw_attention(qkv, grid_h, grid_w, win_h, win_w, heads, params: dict, out=None,
@@ -290,6 +294,7 @@ def ilw_attention(qkv, grid_h, grid_w, win_h, win_w, heads, params: dict, out=No
     """qkv int8 [B, T, 3D] -> out int8 [B, T, D]."""
     B, T, D3 = qkv.shape
     D = D3 // 3
+    _int32("ilw_attention", grid_h, grid_w, win_h, win_w, heads)
     if out is None:
         out = torch.empty((B, T, D), dtype=torch.int8, device=qkv.device)
     need = lib().ilw_attention_workspace_bytes(B, grid_h, grid_w, win_h, win_w, D, D // heads)
@@ -325,6 +330,10 @@ class DeviceBlock:
             assert self.t[k].dtype == dt, (k, self.t[k].dtype)
         t = self.t
         s = BlockParams()
+        for n in ("dim", "heads", "head_dim", "mlp_dim", "ln_iters", "res1_mult_a", "res1_mult_b",
+                  "res1_shift", "gelu_I0", "gelu_k_inter", "gelu_k_out", "gelu_mult", "gelu_shift",
+                  "res2_mult_a", "res2_mult_b", "res2_shift"):
+            _int32(n, int(p[n]))
         s.dim, s.heads, s.head_dim = int(p["dim"]), int(p["heads"]), int(p["head_dim"])
         s.mlp_dim, s.ln_iters = int(p["mlp_dim"]), int(p["ln_iters"])
         s.ln1_beta = t["ln1_beta"].data_ptr()
@@ -350,6 +359,7 @@ class DeviceBlock:
         self.struct = s
 
     def workspace_bytes(self, B, grid_h, grid_w, win_h, win_w) -> int:
+        _int32("ilw_block_workspace_bytes", B, grid_h, grid_w, win_h, win_w)
         n = lib().ilw_block_workspace_bytes(ctypes.byref(self.struct), B, grid_h, grid_w,
                                             win_h, win_w)
         if n == 0 and B > 0:
@@ -361,6 +371,7 @@ def ilw_block_forward(block: DeviceBlock, x, grid_h, grid_w, win_h, win_w, y=Non
                       workspace=None):
     """x int8 [B, T, D] -> y int8 [B, T, D] (y may be x)."""
     B = x.shape[0]
+    _int32("ilw_block_forward", grid_h, grid_w, win_h, win_w)
     if y is None:
         y = torch.empty_like(x)
     if workspace is None:
@@ -379,6 +390,7 @@ def ilw_block_forward_noalloc(block: DeviceBlock, x, grid_h, grid_w, win_h, win_
     argument; the library allocates nothing).  y must be given by callers
     that cannot allocate."""
     B = x.shape[0]
+    _int32("ilw_block_forward_noalloc", grid_h, grid_w, win_h, win_w)
     if y is None:
         y = torch.empty_like(x)
     rc = lib().ilw_block_forward_noalloc(ctypes.byref(block.struct), _dev(x, torch.int8, "x"),
@@ -400,6 +412,7 @@ class Encoder:
                        for b in blocks]
         self.windows = [tuple(int(v) for v in w) for w in windows]
         assert len(self.windows) == len(self.blocks)
+        _int32("Encoder", grid_h, grid_w)
         self.grid_h, self.grid_w = grid_h, grid_w
         self.device = device
         n = len(self.blocks)
@@ -468,6 +481,7 @@ def ilw_patch_embed(img, w, bias, mult, shift, pos, pos_mult_a, pos_mult_b, pos_
     positional embedding pos int8 [T, D] added."""
     B, C, H, W = img.shape
     D = w.shape[0]
+    _int32("ilw_patch_embed", patch, pos_mult_a, pos_mult_b, pos_shift)
     T = (H // patch) * (W // patch)
     if y is None:
         y = torch.empty((B, T, D), dtype=torch.int8, device=img.device)
@@ -482,6 +496,7 @@ def ilw_patch_embed(img, w, bias, mult, shift, pos, pos_mult_a, pos_mult_b, pos_
 
 def ilw_shiftmax_ivit(x, I0, M=31, k_inter=16, k_out=8, y=None):
     """I-ViT Shiftmax (fixed division precision M) of every row of int8 x."""
+    _int32("ilw_shiftmax_ivit", I0, k_inter, k_out, M)
     cols = x.shape[-1]
     rows = x.numel() // cols
     if y is None:
@@ -493,6 +508,7 @@ def ilw_shiftmax_ivit(x, I0, M=31, k_inter=16, k_out=8, y=None):
 
 def ilw_shiftgelu_ivit(x, I0, out_mult, out_shift, k_inter=16, k_out=8, y=None):
     """I-ViT ShiftGELU (row-maximum shift) of every row of int8 x, requantized."""
+    _int32("ilw_shiftgelu_ivit", I0, k_inter, k_out, out_mult, out_shift)
     cols = x.shape[-1]
     rows = x.numel() // cols
     if y is None:
@@ -519,7 +535,9 @@ class DeviceDecoder:
                   "gelu_k_out", "gelu_mult", "gelu_shift", "res1_mult_a", "res1_mult_b",
                   "res1_shift", "res2_mult_a", "res2_mult_b", "res2_shift", "res3_mult_a",
                   "res3_mult_b", "res3_shift"):
+            _int32(n, int(p[n]))
             setattr(s, n, int(p[n]))
+        _int32("ref_dims", int(p.get("ref_dims", 2)))
         s.ref_dims = int(p.get("ref_dims", 2))
         for stem in ("qkv", "o", "val", "off", "attw", "co", "fc1", "fc2"):
             setattr(s, "w_" + stem, self.t["w_" + stem].data_ptr())
@@ -593,6 +611,7 @@ def _deform(entry, ref_dims, value, level_hw, level_start, ref, offsets, logits,
     _, Q, _, L, P, _ = offsets.shape
     if tuple(ref.shape) != (B, Q, ref_dims):
         raise ValueError(f"ref has shape {tuple(ref.shape)}, expected {(B, Q, ref_dims)}")
+    _int32(entry, I0, k_inter, k_out, m_p, s_d, out_mult, out_shift, mode)
     hw = np.ascontiguousarray(np.asarray(level_hw, np.int32).reshape(L, 2))
     st = np.ascontiguousarray(np.asarray(level_start, np.int32).reshape(L))
     if out is None:
@@ -726,6 +745,7 @@ def ilw_cache_append(cache: KVCache, qkv, heads, cu_new, past, max_new, rope=Non
     or None (no rotation) -> q int8 [T, heads, head_dim], q_scale int32 [T,
     heads]; keys and values go to the cache."""
     dev, D = _device(cache.k, "the cache"), cache.head_dim
+    _int32("ilw_cache_append", heads, max_new)
     if qkv.dim() != 2 or qkv.shape[1] != (heads + 2 * cache.kv_heads) * D:
         raise IlwError(f"qkv must be [tokens, {(heads + 2 * cache.kv_heads) * D}], got "
                        f"{tuple(qkv.shape)}")
@@ -769,6 +789,10 @@ def ilw_cache_attention(cache: KVCache, q, q_scale, cu_q, lens, params: dict, ma
         out = q.new_empty((T, heads * D))
     elif out.numel() != T * heads * D:
         raise IlwError(f"out must have {T * heads * D} elements, got {out.numel()}")
+    ap = CacheAttnParams.from_buffer_copy(_int32(
+        "ilw_cache_attention", params["score_mult"], params["score_shift"], params["out_mult"],
+        params["out_shift"], causal, window))
+    _int32("ilw_cache_attention", max_q, max_len)
     L = lib()
     if workspace is None:
         need = L.ilw_cache_attention_workspace_bytes(cache.struct, cache.seqs, max_q, max_len,
@@ -776,8 +800,6 @@ def ilw_cache_attention(cache: KVCache, q, q_scale, cu_q, lens, params: dict, ma
         if need == 0 and last_error():
             raise IlwError(f"ilw_cache_attention_workspace_bytes: {last_error()}")
         workspace = torch.empty(need, dtype=torch.int8, device=q.device) if need else None
-    ap = CacheAttnParams(params["score_mult"], params["score_shift"], params["out_mult"],
-                         params["out_shift"], causal, window)
     rc = L.ilw_cache_attention(
         cache.struct, _at(q, torch.int8, "q", dev), _at(q_scale, torch.int32, "q_scale", dev),
         _at(cu_q, torch.int32, "cu_q", dev), _at(lens, torch.int32, "lens", dev),
