@@ -393,13 +393,16 @@ hipError_t launch_cfg(const ScaledArgs& a, hipStream_t s) {
 //     against 11.3).  32 channels up to 256 workgroups of them (64 rows of 4096 x
 //     2048: 6.3, 64 channels 7.5).
 //   64 rows: up to 64 rows an expert, or up to 512 workgroups (2048 rows of 1024 x
-//     1024: 10.4, tiles 14.0; 1024 rows of 4096 x 2048: 26.3 against 21.0).  Two waves
-//     from 1024 workgroups on (4096 rows of 64 experts, 2048 x 1024: 47.3, four 51.8;
-//     64 rows of 32768 x 4096: 37.4 against 36.5).
+//     1024: 10.6, tiles of 128 x 128 13.5; 1024 rows of 4096 x 2048: 27.5 against 20.9).
+//     Two waves from 1024 workgroups on (4096 rows of 64 experts, 2048 x 1024: 47.3, four
+//     51.8; 64 rows of 32768 x 4096: 37.4 against 36.5).
 //   More: tiles as of the linears grouped by expert, whose launch has both sides.  Up to
 //     256 of 128 x 128, one a CU, load three steps ahead (4096 rows of 1024 x 8192: 48.4,
 //     one step 66; 700 rows of 4096 x 4096: 26.8 and 29.8); more of them load one, so
 //     that a CU has two (2048 rows of 4096 x 4096: 44.6, three steps 59.6).
+// An expert with many more rows than the average has its weights read again, from L2, for
+// each tile of them (512 rows of 64 experts, 503 of them one's, 2048 x 1024: 11.0, 512
+// rows of one expert in its own tiles 8.8).
 template <int BYTES>
 hipError_t launch_bytes(const ScaledArgs& a, hipStream_t s) {
   // (every grid below 2^32 threads: the entry point holds (M / 64 + E) (N / 128 + 1)
